@@ -101,7 +101,7 @@ def _log(rng, lo, hi):
 def draw(rng):
     op = rng.choice(["norm", "norm-grad", "product", "experts", "clip"])
     if op in ("norm", "norm-grad"):
-        D = rng.choice([64, 768, 1024, 2048, 2880, 4096, 7168, _log(rng, 60, 9000)])
+        D = rng.choice([64, 768, 1024, 2048, 2880, 4096, 7168, _log(rng, 60, 8000)])
         T = _log(rng, 1, min(32768, (16384 * 2880 if op == "norm" else 8192 * 7168) // D))
         make = _norm if op == "norm" else _norm_grad
         post, pre = rng.choice([(True, True), (True, True), (False, True), (True, False)])
