@@ -362,6 +362,95 @@ int llep_zero_absent_gradients(const llep_plan_params *params,
                                float *dw_up, float *dw_down,
                                hipStream_t stream);
 
+/* ---- around the block ------------------------------------------------------
+ * What stands between one block of a transformer and the next: the norm of
+ * the block's output, its gate and residual scale, the residual sum, and the
+ * norm before the next block. With rms(v) = 1 / sqrt(mean(v^2) + eps), for
+ * every row t (a token):
+ *   n[t] = b[t] * rms(b[t]) * w_post      (w_post null: n = b)
+ *   r[t] = x[t] + alpha * g[t] * n[t]     (b null: r = x)
+ *   h[t] = r[t] * rms(r[t]) * w_pre       (w_pre null: no h)
+ * in float32, r and h rounded once to dtype (h from the r before rounding).
+ */
+
+/* Shape of the gate g: none (1), one value per channel [D], per token [T], or
+ * per element [T][D]; broadcast along the missing axis. */
+typedef enum {
+  LLEP_GATE_NONE = 0,
+  LLEP_GATE_CHANNEL = 1,
+  LLEP_GATE_TOKEN = 2,
+  LLEP_GATE_FULL = 3
+} llep_gate_shape;
+
+#define LLEP_MAX_NORM_DIM 8192 /* largest D of the norm calls */
+
+/* x, b, r, h [T][D], gate, w_post [D] and w_pre [D] in dtype, any D up to
+ * LLEP_MAX_NORM_DIM and any alignment that the type has by itself (rows of
+ * whole 16-byte vectors that start on 16-byte boundaries run fastest).
+ * Outputs, null where not wanted: r; h; and h_q [T][q_bytes] with h_scale [T],
+ * h as the 8-bit rows of llep_quantize_rows (taken before h is rounded;
+ * q_bytes a multiple of 64, at least D). r may be x, and h may be x or b.
+ * Errors: LLEP_E_ARG (sizes, nulls, a gate or w_post without b, h or h_q
+ * without w_pre, r missing with nothing else wanted), LLEP_E_DTYPE. */
+int llep_block_norm(int64_t T, int32_t D, llep_dtype dtype, const void *x,
+                    const void *b, const void *gate, llep_gate_shape gate_shape,
+                    const void *w_post, const void *w_pre, float alpha,
+                    float eps, void *r, void *h, int8_t *h_q, float *h_scale,
+                    int32_t q_bytes, hipStream_t stream);
+
+/* Backward of llep_block_norm for the same b, gate, weights, alpha and eps,
+ * and its r (read where w_pre is given). d_r [T][D]: the gradient that reaches
+ * r by the residual stream, d_h [T][D] the one of h (null without w_pre).
+ * With i_r = rms(r), i_b = rms(b) (1 without w_post), e = d_h * w_pre:
+ *   dx = d_r + i_r e - i_r^3 r mean(e r),   m = alpha g dx,   f = m w_post
+ *   db = i_b f - i_b^3 b mean(f b)          (without w_post: db = m)
+ *   dw_pre = sum_t d_h r i_r,  dw_post = sum_t m b i_b,
+ *   d_gate = alpha dx n, summed over the axis that the gate is broadcast along.
+ * dx, db in dtype (db null without b; dx may be d_r or d_h, db may be d_h);
+ * d_gate (the gate's shape), dw_post, dw_pre float32, sums in a fixed order;
+ * each null where the forward had no such input. Workspace of at least
+ * llep_block_norm_backward_workspace_bytes(T, D) bytes (0 for invalid sizes),
+ * 16-byte aligned.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE, LLEP_E_WORKSPACE. */
+size_t llep_block_norm_backward_workspace_bytes(int64_t T, int32_t D);
+int llep_block_norm_backward(int64_t T, int32_t D, llep_dtype dtype,
+                             const void *r, const void *b, const void *gate,
+                             llep_gate_shape gate_shape, const void *w_post,
+                             const void *w_pre, float alpha, float eps,
+                             const void *d_r, const void *d_h, void *dx,
+                             void *db, float *d_gate, float *dw_post,
+                             float *dw_pre, void *workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
+/* One tensor of a list of gradients: n elements in dtype, dense. `data` and
+ * `out` are device pointers; the array of descriptors is host memory, read
+ * during the call only. */
+typedef struct {
+  const void *data;
+  void *out; /* clipped gradient (may be data); not read by llep_gradient_norm */
+  int64_t n; /* >= 0 */
+  int32_t dtype; /* llep_dtype */
+  int32_t reserved; /* must be 0 */
+} llep_gradient;
+
+/* norm[0] = sqrt of the sum of g^2 over all elements of all n tensors, summed
+ * in 64 bits in a fixed order (no float32 gradient overflows it).
+ * llep_clip_gradients also writes, with that norm,
+ *   out = g * min(1, max_norm / norm)
+ * (in 32 bits, rounded once to the tensor's dtype). A norm that is infinite or
+ * NaN, or at most max_norm, leaves every gradient as it is: norm tells the
+ * caller, who then skips the step. Outputs may be the inputs, but may not
+ * overlap them otherwise, nor each other. No tensors: norm = 0. Workspace of
+ * llep_clip_gradients_workspace_bytes() bytes, 16-byte aligned, for both.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE, LLEP_E_WORKSPACE. */
+size_t llep_clip_gradients_workspace_bytes(void);
+int llep_gradient_norm(int32_t n, const llep_gradient *grads, float *norm,
+                       void *workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+int llep_clip_gradients(int32_t n, const llep_gradient *grads, float max_norm,
+                        float *norm, void *workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
 /* Text of the calling thread's last error ("" if none). */
 const char *llep_last_error(void);
 

@@ -17,6 +17,13 @@ from .backward import (  # noqa: F401
     silu_grad,
     swiglu_ffn_backward,
 )
+from .block import (  # noqa: F401
+    block_norm,
+    block_norm_backward,
+    clip_gradients,
+    gradient_norm,
+    rms_norm,
+)
 from .llep import (  # noqa: F401
     DeviceLedger,
     PlanResult,

@@ -29,6 +29,8 @@ LLEP_STATUS_FFN_WAIT = 2
 LLEP_MAX_EXPERTS = 512
 LLEP_MAX_DEVICES = 64
 LLEP_MAX_FFN_DIM = 65536
+LLEP_MAX_NORM_DIM = 8192
+LLEP_GATE_NONE, LLEP_GATE_CHANNEL, LLEP_GATE_TOKEN, LLEP_GATE_FULL = range(4)
 
 EXPORTED = [
     "llep_plan", "llep_permute", "llep_grouped_ffn", "llep_combine",
@@ -37,7 +39,9 @@ EXPORTED = [
     "llep_packed_down_bytes", "llep_last_error", "llep_combine_backward",
     "llep_pack_weights_backward", "llep_grouped_ffn_backward_workspace_bytes",
     "llep_grouped_ffn_backward", "llep_grouped_ffn_train", "llep_grouped_ffn_noalloc",
-    "llep_zero_absent_gradients",
+    "llep_zero_absent_gradients", "llep_block_norm",
+    "llep_block_norm_backward_workspace_bytes", "llep_block_norm_backward",
+    "llep_clip_gradients_workspace_bytes", "llep_gradient_norm", "llep_clip_gradients",
 ]
 LLEP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -64,6 +68,11 @@ class llep_plan_buffers(ctypes.Structure):
         "group_begin", "device_rows", "xfers", "rank_base", "info")]
 
 
+class llep_gradient(ctypes.Structure):
+    _fields_ = [("data", _P), ("out", _P), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 class LLEPError(RuntimeError):
     def __init__(self, code: int, where: str, msg: str):
         super().__init__(f"{where} failed with code {code}: {msg}")
@@ -83,7 +92,9 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         pp = ctypes.POINTER(llep_plan_params)
         pb = ctypes.POINTER(llep_plan_buffers)
+        pg = ctypes.POINTER(llep_gradient)
         i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        f32 = ctypes.c_float
         sigs = {
             "llep_plan_max_chunks": (i32, [pp]),
             "llep_plan_rank_base_elems": (i64, [pp]),
@@ -111,6 +122,15 @@ def lib() -> ctypes.CDLL:
                                                          i32, i32, ctypes.c_int, _P, _P, _P, _P,
                                                          _P, sz, _P]),
             "llep_zero_absent_gradients": (ctypes.c_int, [pp, pb, i32, i32, i32, _P, _P, _P, _P]),
+            "llep_block_norm": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, _P, _P, ctypes.c_int,
+                                               _P, _P, f32, f32, _P, _P, _P, _P, i32, _P]),
+            "llep_block_norm_backward_workspace_bytes": (sz, [i64, i32]),
+            "llep_block_norm_backward": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, _P, _P,
+                                                        ctypes.c_int, _P, _P, f32, f32, _P, _P,
+                                                        _P, _P, _P, _P, _P, _P, sz, _P]),
+            "llep_clip_gradients_workspace_bytes": (sz, []),
+            "llep_gradient_norm": (ctypes.c_int, [i32, pg, _P, _P, sz, _P]),
+            "llep_clip_gradients": (ctypes.c_int, [i32, pg, f32, _P, _P, sz, _P]),
             "llep_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sigs.items():
@@ -335,3 +355,128 @@ def llep_zero_absent_gradients(params: llep_plan_params, bufs: PlanBuffers, devi
     _check(lib().llep_zero_absent_gradients(
         ctypes.byref(params), ctypes.byref(bufs.struct), device, D, F, _ptr(dw_gate),
         _ptr(dw_up), _ptr(dw_down), _stream(stream)), "llep_zero_absent_gradients")
+
+
+# ---- around the block ------------------------------------------------------------
+
+def _dense(what: str, t, shape, dtype):
+    """t, if it is a dense GPU tensor of this shape and type (or None)."""
+    if t is None:
+        return t
+    if t.dtype != dtype:
+        raise TypeError(f"{what} is {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} is not contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on a GPU")
+    return t
+
+
+def _gate_shape(gate, T: int, D: int, shape) -> int:
+    """LLEP_GATE_* of a gate of shape [1, D] or [D], [T, 1], or [T, D] (or None)."""
+    if gate is None:
+        return LLEP_GATE_NONE
+    if shape is not None:
+        return shape
+    if tuple(gate.shape) in ((1, D), (D,)):
+        return LLEP_GATE_CHANNEL
+    if tuple(gate.shape) == (T, 1):
+        return LLEP_GATE_TOKEN
+    if tuple(gate.shape) == (T, D):
+        return LLEP_GATE_FULL
+    raise ValueError(f"gate of shape {tuple(gate.shape)} fits no rows of [{T}, {D}]")
+
+
+def llep_block_norm(x, b, gate, w_post, w_pre, alpha: float, eps: float, r, h=None, h_q=None,
+                    h_scale=None, stream=None, gate_shape=None):
+    """r = x + alpha * gate * norm(b) * w_post, h = norm(r) * w_pre (see llep.h). x, b, r, h
+    [T, D]; gate None, [1, D], [T, 1] or [T, D] (gate_shape: LLEP_GATE_*, where the shape alone
+    leaves it open); h_q [T, bytes] int8 with h_scale [T]: h as 8-bit rows. Any of b, gate,
+    w_post, w_pre, and outputs, may be None."""
+    import torch
+    T, D = x.shape
+    dt = x.dtype
+    code = _dtype_code(x)
+    shape = _gate_shape(gate, T, D, gate_shape)
+    for what, t in (("x", x), ("b", b), ("r", r), ("h", h)):
+        _dense(what, t, (T, D), dt)
+    for what, t in (("w_post", w_post), ("w_pre", w_pre)):
+        _dense(what, t, (D,), dt)
+    if gate is not None:
+        _dense("gate", gate, gate.shape, dt)
+    q_bytes = 0
+    if h_q is not None:
+        q_bytes = h_q.shape[-1]
+        _dense("h_q", h_q, (T, q_bytes), torch.int8)
+        _dense("h_scale", h_scale, (T,), torch.float32)
+    _check(lib().llep_block_norm(T, D, code, _ptr(x), _ptr(b), _ptr(gate), shape, _ptr(w_post),
+                                 _ptr(w_pre), alpha, eps, _ptr(r), _ptr(h), _ptr(h_q),
+                                 _ptr(h_scale), q_bytes, _stream(stream)), "llep_block_norm")
+
+
+def llep_block_norm_backward_workspace_bytes(T: int, D: int) -> int:
+    return lib().llep_block_norm_backward_workspace_bytes(T, D)
+
+
+def llep_block_norm_backward(r, b, gate, w_post, w_pre, alpha: float, eps: float, d_r, d_h, dx,
+                             db, d_gate, dw_post, dw_pre, workspace, stream=None,
+                             gate_shape=None):
+    """Every gradient of llep_block_norm (see llep.h): dx, db in x's type; d_gate (the gate's
+    shape), dw_post, dw_pre float32; None for inputs that the forward had not."""
+    import torch
+    T, D = d_r.shape
+    dt = d_r.dtype
+    code = _dtype_code(d_r)
+    shape = _gate_shape(gate, T, D, gate_shape)
+    for what, t in (("r", r), ("b", b), ("d_r", d_r), ("d_h", d_h), ("dx", dx), ("db", db)):
+        _dense(what, t, (T, D), dt)
+    for what, t in (("w_post", w_post), ("w_pre", w_pre)):
+        _dense(what, t, (D,), dt)
+    for what, t in (("dw_post", dw_post), ("dw_pre", dw_pre)):
+        _dense(what, t, (D,), torch.float32)
+    if gate is not None:
+        _dense("gate", gate, gate.shape, dt)
+        _dense("d_gate", d_gate, gate.shape, torch.float32)
+    _check(lib().llep_block_norm_backward(
+        T, D, code, _ptr(r), _ptr(b), _ptr(gate), shape, _ptr(w_post), _ptr(w_pre), alpha, eps,
+        _ptr(d_r), _ptr(d_h), _ptr(dx), _ptr(db), _ptr(d_gate), _ptr(dw_post), _ptr(dw_pre),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+        "llep_block_norm_backward")
+
+
+def llep_clip_gradients_workspace_bytes() -> int:
+    return lib().llep_clip_gradients_workspace_bytes()
+
+
+def _gradients(grads, out):
+    """The llep_gradient array of dense bf16 / float32 tensors."""
+    if len(out) != len(grads):
+        raise ValueError("as many outputs as gradients")
+    table = (llep_gradient * max(len(grads), 1))()
+    for i, (g, o) in enumerate(zip(grads, out)):
+        _dense(f"gradient {i}", g, g.shape, g.dtype)
+        _dense(f"output {i}", o, g.shape, g.dtype)
+        table[i] = llep_gradient(_ptr(g), _ptr(o), g.numel(), _dtype_code(g), 0)
+    return table
+
+
+def llep_gradient_norm(grads, norm, workspace, stream=None):
+    """norm [1] float32 = the 2-norm over all elements of the tensors."""
+    import torch
+    _dense("norm", norm, (1,), torch.float32)
+    _check(lib().llep_gradient_norm(len(grads), _gradients(grads, grads), _ptr(norm),
+                                    _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                    _stream(stream)), "llep_gradient_norm")
+
+
+def llep_clip_gradients(grads, max_norm: float, norm, workspace, out=None, stream=None):
+    """llep_gradient_norm, then every gradient times min(1, max_norm / norm), in place or into
+    `out` (tensors of the same shapes and types)."""
+    import torch
+    _dense("norm", norm, (1,), torch.float32)
+    _check(lib().llep_clip_gradients(len(grads), _gradients(grads, grads if out is None else out),
+                                     max_norm, _ptr(norm), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "llep_clip_gradients")

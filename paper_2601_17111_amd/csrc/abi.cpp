@@ -74,6 +74,51 @@ int check_ffn_dims(int32_t D, int32_t F, llep_dtype dtype) {
   return LLEP_OK;
 }
 
+bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// the arguments that the block norm and its backward share
+int check_norm(int64_t T, int32_t D, llep_dtype dtype, const void *b, const void *gate,
+               llep_gate_shape gate_shape, const void *w_post, const void *w_pre, float eps) {
+  const size_t eb = elem_bytes(dtype);
+  if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  if (T < 0) return fail(LLEP_E_ARG, "T < 0");
+  if (D < 1 || D > LLEP_MAX_NORM_DIM) return fail(LLEP_E_ARG, "D outside [1, LLEP_MAX_NORM_DIM]");
+  if (!(eps >= 0.0f)) return fail(LLEP_E_ARG, "eps < 0");
+  if (gate_shape < LLEP_GATE_NONE || gate_shape > LLEP_GATE_FULL)
+    return fail(LLEP_E_ARG, "unknown gate shape");
+  if ((gate != nullptr) != (gate_shape != LLEP_GATE_NONE) &&
+      !(T == 0 && gate_shape > LLEP_GATE_CHANNEL))
+    return fail(LLEP_E_ARG, "gate and gate_shape do not agree");
+  if (!b && T > 0 && (gate_shape != LLEP_GATE_NONE || w_post))
+    return fail(LLEP_E_ARG, "a gate or w_post without b");
+  if (!aligned_to(b, eb) || !aligned_to(gate, eb) || !aligned_to(w_post, eb) ||
+      !aligned_to(w_pre, eb))
+    return fail(LLEP_E_ARG, "data not aligned to its type");
+  return LLEP_OK;
+}
+
+int check_gradients(int32_t n, const llep_gradient *grads, bool scale, const float *norm,
+                    const void *workspace, size_t workspace_bytes) {
+  if (n < 0) return fail(LLEP_E_ARG, "n < 0");
+  if (n > 0 && !grads) return fail(LLEP_E_ARG, "grads is null");
+  if (!norm || !aligned_to(norm, 4)) return fail(LLEP_E_ARG, "norm is null or not aligned");
+  for (int32_t i = 0; i < n; ++i) {
+    const llep_gradient &g = grads[i];
+    const size_t eb = elem_bytes(llep_dtype(g.dtype));
+    if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+    if (g.n < 0) return fail(LLEP_E_ARG, "a tensor of fewer than 0 elements");
+    if (g.reserved != 0) return fail(LLEP_E_ARG, "reserved field is not 0");
+    if (g.n > 0 && (!g.data || (scale && !g.out))) return fail(LLEP_E_ARG, "a data pointer is null");
+    if (!aligned_to(g.data, eb) || (scale && !aligned_to(g.out, eb)))
+      return fail(LLEP_E_ARG, "data not aligned to its type");
+  }
+  if (!workspace || workspace_bytes < llep_clip_gradients_workspace_bytes())
+    return fail(LLEP_E_WORKSPACE,
+                "workspace missing or smaller than llep_clip_gradients_workspace_bytes");
+  if (!aligned16(workspace)) return fail(LLEP_E_WORKSPACE, "workspace not 16-byte aligned");
+  return LLEP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -408,6 +453,118 @@ int llep_zero_absent_gradients(const llep_plan_params *params, const llep_plan_b
   a.dw_up = dw_up;
   a.dw_down = dw_down;
   return hip_result(llep::launch_zero_absent(a, stream), "llep_zero_absent_gradients");
+}
+
+int llep_block_norm(int64_t T, int32_t D, llep_dtype dtype, const void *x, const void *b,
+                    const void *gate, llep_gate_shape gate_shape, const void *w_post,
+                    const void *w_pre, float alpha, float eps, void *r, void *h, int8_t *h_q,
+                    float *h_scale, int32_t q_bytes, hipStream_t stream) {
+  int rc = check_norm(T, D, dtype, b, gate, gate_shape, w_post, w_pre, eps);
+  if (rc != LLEP_OK) return rc;
+  if ((h || h_q) && !w_pre) return fail(LLEP_E_ARG, "h or h_q without w_pre");
+  if ((h_q != nullptr) != (h_scale != nullptr)) return fail(LLEP_E_ARG, "h_q without h_scale");
+  if (h_q && (q_bytes < D || q_bytes % 64 != 0))
+    return fail(LLEP_E_ARG, "q_bytes must be a multiple of 64, at least D");
+  if (h_q && (!aligned16(h_q) || !aligned_to(h_scale, 4)))
+    return fail(LLEP_E_ARG, "h_q / h_scale not aligned");
+  const size_t eb = elem_bytes(dtype);
+  if (!aligned_to(x, eb) || !aligned_to(r, eb) || !aligned_to(h, eb))
+    return fail(LLEP_E_ARG, "data not aligned to its type");
+  if (T > 0 && !x) return fail(LLEP_E_ARG, "x is null");
+  if (T > 0 && !r && !h && !h_q) return fail(LLEP_E_ARG, "no output");
+  llep::NormArgs a = {};
+  a.T = T;
+  a.D = D;
+  a.dtype = dtype;
+  a.gate_shape = gate_shape;
+  a.alpha = alpha;
+  a.eps = eps;
+  a.x = x;
+  a.b = b;
+  a.gate = gate;
+  a.w_post = w_post;
+  a.w_pre = h || h_q ? w_pre : nullptr;
+  a.r = r;
+  a.h = h;
+  a.h_q = h_q;
+  a.h_scale = h_scale;
+  a.q_bytes = q_bytes;
+  return hip_result(llep::launch_block_norm(a, stream), "llep_block_norm");
+}
+
+size_t llep_block_norm_backward_workspace_bytes(int64_t T, int32_t D) {
+  if (T < 0 || D < 1 || D > LLEP_MAX_NORM_DIM) return 0;
+  return llep::norm_bwd_workspace_bytes(T, D);
+}
+
+int llep_block_norm_backward(int64_t T, int32_t D, llep_dtype dtype, const void *r, const void *b,
+                             const void *gate, llep_gate_shape gate_shape, const void *w_post,
+                             const void *w_pre, float alpha, float eps, const void *d_r,
+                             const void *d_h, void *dx, void *db, float *d_gate, float *dw_post,
+                             float *dw_pre, void *workspace, size_t workspace_bytes,
+                             hipStream_t stream) {
+  int rc = check_norm(T, D, dtype, b, gate, gate_shape, w_post, w_pre, eps);
+  if (rc != LLEP_OK) return rc;
+  const size_t eb = elem_bytes(dtype);
+  if (T > 0 && (!d_r || !dx)) return fail(LLEP_E_ARG, "d_r or dx is null");
+  if (T > 0 && (w_pre != nullptr) != (d_h != nullptr))
+    return fail(LLEP_E_ARG, "d_h and w_pre: both or none");
+  if (T > 0 && w_pre && !r) return fail(LLEP_E_ARG, "r is null");
+  if (T > 0 && (b != nullptr) != (db != nullptr)) return fail(LLEP_E_ARG, "db and b: both or none");
+  if ((w_pre != nullptr) != (dw_pre != nullptr) || (w_post != nullptr) != (dw_post != nullptr))
+    return fail(LLEP_E_ARG, "dw_pre (dw_post) and w_pre (w_post): both or none");
+  if ((gate_shape == LLEP_GATE_NONE) != (d_gate == nullptr) &&
+      !(T == 0 && gate_shape > LLEP_GATE_CHANNEL))
+    return fail(LLEP_E_ARG, "d_gate and gate_shape do not agree");
+  if (!aligned_to(r, eb) || !aligned_to(d_r, eb) || !aligned_to(d_h, eb) || !aligned_to(dx, eb) ||
+      !aligned_to(db, eb) || !aligned_to(d_gate, 4) || !aligned_to(dw_post, 4) ||
+      !aligned_to(dw_pre, 4))
+    return fail(LLEP_E_ARG, "data not aligned to its type");
+  if (workspace_bytes < llep_block_norm_backward_workspace_bytes(T, D) || (T > 0 && !workspace))
+    return fail(LLEP_E_WORKSPACE,
+                "workspace missing or smaller than llep_block_norm_backward_workspace_bytes");
+  if (!aligned16(workspace)) return fail(LLEP_E_WORKSPACE, "workspace not 16-byte aligned");
+  llep::NormBwdArgs a = {};
+  a.n.T = T;
+  a.n.D = D;
+  a.n.dtype = dtype;
+  a.n.gate_shape = gate_shape;
+  a.n.alpha = alpha;
+  a.n.eps = eps;
+  a.n.b = b;
+  a.n.gate = gate;
+  a.n.w_post = w_post;
+  a.n.w_pre = w_pre;
+  a.r = r;
+  a.d_r = d_r;
+  a.d_h = d_h;
+  a.dx = dx;
+  a.db = db;
+  a.d_gate = d_gate;
+  a.dw_post = dw_post;
+  a.dw_pre = dw_pre;
+  a.parts = static_cast<float *>(workspace);
+  a.column_sums = dw_post || gate_shape == LLEP_GATE_CHANNEL;
+  return hip_result(llep::launch_block_norm_backward(a, stream), "llep_block_norm_backward");
+}
+
+size_t llep_clip_gradients_workspace_bytes(void) { return llep::kClipParts * sizeof(double); }
+
+int llep_gradient_norm(int32_t n, const llep_gradient *grads, float *norm, void *workspace,
+                       size_t workspace_bytes, hipStream_t stream) {
+  const int rc = check_gradients(n, grads, false, norm, workspace, workspace_bytes);
+  if (rc != LLEP_OK) return rc;
+  llep::ClipArgs a = {n, grads, 0.0f, false, norm, static_cast<double *>(workspace)};
+  return hip_result(llep::launch_clip(a, stream), "llep_gradient_norm");
+}
+
+int llep_clip_gradients(int32_t n, const llep_gradient *grads, float max_norm, float *norm,
+                        void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!(max_norm >= 0.0f)) return fail(LLEP_E_ARG, "max_norm < 0");
+  const int rc = check_gradients(n, grads, true, norm, workspace, workspace_bytes);
+  if (rc != LLEP_OK) return rc;
+  llep::ClipArgs a = {n, grads, max_norm, true, norm, static_cast<double *>(workspace)};
+  return hip_result(llep::launch_clip(a, stream), "llep_clip_gradients");
 }
 
 }  // extern "C"

@@ -128,6 +128,46 @@ struct CombineBwdArgs {
 };
 hipError_t launch_combine_backward(const CombineBwdArgs &a, hipStream_t stream);
 
+// Norms around a block (norm.hip); b, gate, w_post, w_pre, r, h, h_q may be null.
+struct NormArgs {
+  int64_t T;
+  int32_t D;
+  llep_dtype dtype;
+  llep_gate_shape gate_shape;
+  float alpha, eps;
+  const void *x, *b, *gate, *w_post, *w_pre;
+  void *r, *h;
+  int8_t *h_q;
+  float *h_scale;
+  int32_t q_bytes;  // of a row of h_q
+};
+hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream);
+
+// workgroups of the backward at most (rows of column sums in the workspace)
+constexpr int kNormBwdGrid = 1024;
+struct NormBwdArgs {
+  NormArgs n;  // the forward's b, gate, weights and numbers
+  const void *r, *d_r, *d_h;
+  void *dx, *db;
+  float *d_gate, *dw_post, *dw_pre;
+  float *parts;      // [workgroups][2][D]
+  bool column_sums;  // whether d w_post or d g is summed over the rows
+};
+size_t norm_bwd_workspace_bytes(int64_t T, int32_t D);
+hipError_t launch_block_norm_backward(const NormBwdArgs &a, hipStream_t stream);
+
+// Gradient norm and clipping (clip.hip).
+struct ClipArgs {
+  int32_t n;
+  const llep_gradient *grads;  // host
+  float max_norm;
+  bool scale;  // whether the gradients are clipped, or only their norm taken
+  float *norm;
+  double *parts;  // [kClipParts]
+};
+constexpr int kClipParts = 1024;
+hipError_t launch_clip(const ClipArgs &a, hipStream_t stream);
+
 hipError_t launch_pack(int32_t E, int32_t D, int32_t F, llep_dtype dtype,
                        const void *w_gate, const void *w_up,
                        const void *w_down, void *gu, void *dn,
