@@ -422,6 +422,88 @@ int llep_block_norm_backward(int64_t T, int32_t D, llep_dtype dtype,
                              float *dw_pre, void *workspace,
                              size_t workspace_bytes, hipStream_t stream);
 
+/* ---- 8-bit products ---------------------------------------------------------
+ * Activations and weights as signed bytes with a scale for each token (row)
+ * and each output channel:
+ *   y[m][n] = x_scale[m] * w_scale[n] * sum_k x[m][k] * w[n][k],
+ * the sum exact in 32-bit integers (K is at most LLEP_MAX_FFN_DIM), the scales
+ * applied in float32 in this order: (float(sum) * x_scale) * w_scale.
+ */
+#define LLEP_MAX_INT8_ROWS 0x7fffff00 /* largest M of llep_int8_matmul */
+#define LLEP_MAX_INT8_COLUMNS (1 << 20) /* largest N of an 8-bit matrix */
+
+/* Bytes of an 8-bit row of D values: D rounded up to a multiple of 64 (-1
+ * outside [1, LLEP_MAX_FFN_DIM]). */
+int32_t llep_int8_row_bytes(int32_t D);
+
+/* Rows to 8 bits: scale[r] = max_i |x[r][i]| * (1 / 127),
+ *   q[r][i] = rint(x[r][i] * (127 * (1 / max_i |x[r][i]|)))   (ties to even)
+ * with every step rounded to float32, q[r][D ..] = 0. A row whose largest magnitude is below 2^-120
+ * counts as zero (scale and q are 0). A row with an infinity or a NaN gets
+ * scale NaN and q = 0, so that everything computed from it is NaN. x [R][D] in
+ * dtype, any D up to LLEP_MAX_FFN_DIM; q [R][q_bytes], q_bytes a multiple of
+ * 64, at least D, q 16-byte aligned; scale [R].
+ * Weights are rows too, one per output channel ([N][K]).
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+int llep_quantize_rows(int64_t R, int32_t D, llep_dtype dtype, const void *x,
+                       int8_t *q, int32_t q_bytes, float *scale,
+                       hipStream_t stream);
+
+/* Packed 8-bit weights (untimed setup): per expert (E = 1: one matrix) rows
+ * w[n][k], n < N output channels, in blocks of 16 rows x 64 k: element (n, k)
+ * at ((n/16) * (K'/64) + k/64) * 1024 + (n%16) * 64 + k%64, K' = K rounded up
+ * to a multiple of 64, zeros in rows from N and columns from K on.
+ * w [E][N][K]; with w_up [E][N][K] (N % 32 == 0) the matrix has 2N rows: row
+ * 64j + c is row 32j + c of w (the gate), row 64j + 32 + c row 32j + c of w_up.
+ * packed: llep_packed_int8_bytes(E, N, K) bytes, twice that with w_up; 0 for
+ * sizes outside E <= LLEP_MAX_EXPERTS, N <= LLEP_MAX_INT8_COLUMNS,
+ * K <= LLEP_MAX_FFN_DIM.
+ * Errors: LLEP_E_ARG. */
+size_t llep_packed_int8_bytes(int32_t E, int32_t N, int32_t K);
+int llep_pack_int8(int32_t E, int32_t N, int32_t K, const int8_t *w,
+                   const int8_t *w_up, int8_t *packed, hipStream_t stream);
+
+/* out[m][n] as above for M rows of x, out [M][N] in dtype (rounded once);
+ * x [M][x_bytes] with x_bytes a multiple of 64, at least
+ * llep_int8_row_bytes(K), zero from K on (llep_quantize_rows writes such rows);
+ * w_packed from llep_pack_int8(1, N, K); w_scale [N]. All arrays but x_scale
+ * 16-byte aligned; workspace of at least llep_int8_matmul_workspace_bytes
+ * bytes (which may be 0), 256-byte aligned.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE, LLEP_E_WORKSPACE. */
+size_t llep_int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K);
+int llep_int8_matmul(int64_t M, int32_t N, int32_t K, const int8_t *x,
+                     int32_t x_bytes, const float *x_scale,
+                     const int8_t *w_packed, const float *w_scale,
+                     llep_dtype dtype, void *out, void *workspace,
+                     size_t workspace_bytes, hipStream_t stream);
+
+/* Step 4 with 8-bit weights and activations, for serving. For every group
+ * (device, e, row_start, n) of `device` (or of all devices when -1):
+ *   g = x Wg_e, u = x Wu_e     (8-bit products of the rows of x_perm)
+ *   act = silu(g) * u          (float32), then to 8 bits by row, as
+ *                              llep_quantize_rows
+ *   out_perm = act Wd_e        (8-bit product, rounded once to bfloat16)
+ * x_perm [T*K][D] bytes in plan order (llep_permute moves rows of D bytes as
+ * D/2 bfloat16); x_scale per token: row r has x_scale[row_pair[r] / K], with
+ * row_pair from llep_permute, or x_scale[r] with row_pair null.
+ * w_gate_up_packed: llep_pack_int8(E, F, D) with gate and up rows, gate_scale
+ * and up_scale [E][F]; w_down_packed: llep_pack_int8(E, D, F), down_scale
+ * [E][D]. out_perm [T*K][D] bfloat16, rows outside the range not written.
+ * Requires D % 64 == 0, F % 64 == 0, both at most LLEP_MAX_FFN_DIM; workspace
+ * of at least llep_grouped_ffn_int8_workspace_bytes bytes, 256-byte aligned.
+ * Errors: LLEP_E_ARG, LLEP_E_WORKSPACE. */
+size_t llep_grouped_ffn_int8_workspace_bytes(const llep_plan_params *params,
+                                             int32_t F);
+int llep_grouped_ffn_int8(const llep_plan_params *params,
+                          const llep_plan_buffers *plan, int32_t device,
+                          const int8_t *x_perm, const float *x_scale,
+                          const int32_t *row_pair,
+                          const int8_t *w_gate_up_packed,
+                          const float *gate_scale, const float *up_scale,
+                          const int8_t *w_down_packed, const float *down_scale,
+                          int32_t D, int32_t F, void *out_perm, void *workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
 /* One tensor of a list of gradients: n elements in dtype, dense. `data` and
  * `out` are device pointers; the array of descriptors is host memory, read
  * during the call only. */

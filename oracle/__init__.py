@@ -22,7 +22,10 @@ from .block import (  # noqa: F401
     block_norm_backward,
     clip_gradients,
     gradient_norm,
+    int8_product,
+    quantize_rows,
     rms_norm,
+    swiglu_ffn_int8,
 )
 from .llep import (  # noqa: F401
     DeviceLedger,

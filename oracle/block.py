@@ -13,6 +13,8 @@ from typing import Dict, List, Sequence, Tuple
 
 import numpy as np
 
+from .llep import silu
+
 
 def _f64(a):
     return None if a is None else np.asarray(a, dtype=np.float64)
@@ -72,6 +74,43 @@ def block_norm_backward(r, b, gate, w_post, w_pre, alpha, eps, d_r, d_h) -> Dict
                 d_gate = d_gate.sum(axis=axis, keepdims=True)
         out["d_gate"] = d_gate
     return out
+
+
+def quantize_rows(x) -> Tuple[np.ndarray, np.ndarray]:
+    """8-bit rows in IEEE float32, step by step: scale = most * (1 / 127) and
+    q = rint(x * (127 * (1 / most))) (ties to even) with most = max |x| of the row;
+    rows below 2^-120 count as zero; rows that are not finite: scale NaN, q 0.
+    Returns (q int8, scale float32)."""
+    x = np.asarray(x, dtype=np.float32)
+    q = np.zeros(x.shape, dtype=np.int8)
+    scale = np.zeros(x.shape[0], dtype=np.float32)
+    for t, row in enumerate(x):
+        most = np.abs(row).max() if np.isfinite(row).all() else np.float32(np.nan)
+        if np.isnan(most):
+            scale[t] = np.nan
+        elif most >= np.float32(2.0 ** -120):
+            scale[t] = most * (np.float32(1) / np.float32(127))
+            q[t] = np.rint(row * (np.float32(127) * (np.float32(1) / most))).astype(np.int8)
+    return q, scale
+
+
+def int8_product(x, x_scale, w, w_scale) -> np.ndarray:
+    """x_scale[m] w_scale[n] sum_k x[m][k] w[n][k], the sum in whole numbers."""
+    s = np.asarray(x, dtype=np.int64) @ np.asarray(w, dtype=np.int64).T
+    return s.astype(np.float64) * _f64(x_scale)[:, None] * _f64(w_scale)[None, :]
+
+
+def swiglu_ffn_int8(x, x_scale, w_gate, s_gate, w_up, s_up, w_down, s_down):
+    """One expert on 8-bit rows (weights [F][D], [F][D], [D][F], rows = output
+    channels): float64, the activation to 8 bits by row in between. Returns the
+    outputs and the activations' row maxima."""
+    g = int8_product(x, x_scale, w_gate, s_gate)
+    a = silu(g) * int8_product(x, x_scale, w_up, s_up)
+    most = np.abs(a).max(axis=1, keepdims=True, initial=0.0)
+    step = np.where(most > 0, most / 127.0, 1.0)
+    q = np.rint(a / step)
+    w = _f64(w_down) * _f64(s_down)[:, None]
+    return (q * step) @ w.T, most[:, 0]
 
 
 def gradient_norm(grads: Sequence[np.ndarray]) -> float:

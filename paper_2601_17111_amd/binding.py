@@ -42,6 +42,9 @@ EXPORTED = [
     "llep_zero_absent_gradients", "llep_block_norm",
     "llep_block_norm_backward_workspace_bytes", "llep_block_norm_backward",
     "llep_clip_gradients_workspace_bytes", "llep_gradient_norm", "llep_clip_gradients",
+    "llep_int8_row_bytes", "llep_quantize_rows", "llep_packed_int8_bytes", "llep_pack_int8",
+    "llep_int8_matmul_workspace_bytes", "llep_int8_matmul",
+    "llep_grouped_ffn_int8_workspace_bytes", "llep_grouped_ffn_int8",
 ]
 LLEP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -128,6 +131,16 @@ def lib() -> ctypes.CDLL:
             "llep_block_norm_backward": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, _P, _P,
                                                         ctypes.c_int, _P, _P, f32, f32, _P, _P,
                                                         _P, _P, _P, _P, _P, _P, sz, _P]),
+            "llep_int8_row_bytes": (i32, [i32]),
+            "llep_quantize_rows": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, _P, i32, _P, _P]),
+            "llep_packed_int8_bytes": (sz, [i32, i32, i32]),
+            "llep_pack_int8": (ctypes.c_int, [i32, i32, i32, _P, _P, _P, _P]),
+            "llep_int8_matmul_workspace_bytes": (sz, [i64, i32, i32]),
+            "llep_int8_matmul": (ctypes.c_int, [i64, i32, i32, _P, i32, _P, _P, _P, ctypes.c_int,
+                                                _P, _P, sz, _P]),
+            "llep_grouped_ffn_int8_workspace_bytes": (sz, [pp, i32]),
+            "llep_grouped_ffn_int8": (ctypes.c_int, [pp, pb, i32, _P, _P, _P, _P, _P, _P, _P, _P,
+                                                     i32, i32, _P, _P, sz, _P]),
             "llep_clip_gradients_workspace_bytes": (sz, []),
             "llep_gradient_norm": (ctypes.c_int, [i32, pg, _P, _P, sz, _P]),
             "llep_clip_gradients": (ctypes.c_int, [i32, pg, f32, _P, _P, sz, _P]),
@@ -480,3 +493,99 @@ def llep_clip_gradients(grads, max_norm: float, norm, workspace, out=None, strea
                                      max_norm, _ptr(norm), _ptr(workspace),
                                      workspace.numel() * workspace.element_size(),
                                      _stream(stream)), "llep_clip_gradients")
+
+
+# ---- 8-bit products ----------------------------------------------------------------
+
+def llep_int8_row_bytes(D: int) -> int:
+    """Bytes of an 8-bit row of D values."""
+    n = lib().llep_int8_row_bytes(D)
+    if n < 0:
+        raise LLEPError(LLEP_E_ARG, "llep_int8_row_bytes", "D outside [1, LLEP_MAX_FFN_DIM]")
+    return n
+
+
+def llep_quantize_rows(x, q, scale, stream=None):
+    """x [R, D] to 8 bits by row: q [R, bytes] int8 (bytes a multiple of 64, at least D; zeros
+    past D) and scale [R] float32."""
+    import torch
+    R, D = x.shape
+    code = _dtype_code(x)
+    _dense("x", x, (R, D), x.dtype)
+    _dense("q", q, (R, q.shape[-1]), torch.int8)
+    _dense("scale", scale, (R,), torch.float32)
+    _check(lib().llep_quantize_rows(R, D, code, _ptr(x), _ptr(q), q.shape[-1], _ptr(scale),
+                                    _stream(stream)), "llep_quantize_rows")
+
+
+def llep_pack_matrix_int8(w, w_up=None, stream=None):
+    """Packed copy of 8-bit weights [N, K] or [E, N, K], rows = output channels; with w_up (the
+    same shape) of gate and up rows together (see llep.h). Returns an int8 tensor [E, bytes]."""
+    import torch
+    if w.dim() not in (2, 3):
+        raise ValueError("weights are [N, K] or [E, N, K]")
+    E, N, K = (1, *w.shape) if w.dim() == 2 else w.shape
+    _dense("w", w, w.shape, torch.int8)
+    _dense("w_up", w_up, w.shape, torch.int8)
+    nbytes = lib().llep_packed_int8_bytes(E, N, K) * (1 if w_up is None else 2)
+    out = torch.empty((E, nbytes // E), dtype=torch.int8, device=w.device)
+    _check(lib().llep_pack_int8(E, N, K, _ptr(w), _ptr(w_up), _ptr(out), _stream(stream)),
+           "llep_pack_int8")
+    return out
+
+
+def llep_int8_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib().llep_int8_matmul_workspace_bytes(M, N, K)
+
+
+def llep_int8_matmul(x, x_scale, w_packed, w_scale, out, K: int, workspace=None, stream=None):
+    """out [M, N] (bf16 or float32) = x_scale w_scale (x w^T): x [M, bytes] int8 rows of K values
+    (llep_quantize_rows), w_packed from llep_pack_matrix_int8, x_scale [M], w_scale [N]."""
+    import torch
+    M, N = out.shape
+    code = _dtype_code(out)
+    _dense("x", x, (M, x.shape[-1]), torch.int8)
+    _dense("x_scale", x_scale, (M,), torch.float32)
+    _dense("w_packed", w_packed, (1, lib().llep_packed_int8_bytes(1, N, K)), torch.int8)
+    _dense("w_scale", w_scale, (N,), torch.float32)
+    _dense("out", out, (M, N), out.dtype)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().llep_int8_matmul(M, N, K, _ptr(x), x.shape[-1], _ptr(x_scale), _ptr(w_packed),
+                                  _ptr(w_scale), code, _ptr(out), _ptr(workspace), nbytes,
+                                  _stream(stream)), "llep_int8_matmul")
+
+
+def llep_grouped_ffn_int8_workspace_bytes(params: llep_plan_params, F: int) -> int:
+    return lib().llep_grouped_ffn_int8_workspace_bytes(ctypes.byref(params), F)
+
+
+def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: int, x_perm,
+                          x_scale, row_pair, w_gate_up, gate_scale, up_scale, w_down, down_scale,
+                          out_perm, workspace, stream=None):
+    """The grouped FFN on 8-bit rows and weights (see llep.h): x_perm [T*K, D] int8, x_scale [T]
+    with row_pair [T*K] int32, or [T*K] with row_pair None; weights from llep_pack_matrix_int8,
+    scales [E, F], [E, F] and [E, D]; out_perm [T*K, D] bf16."""
+    import torch
+    R = params.T * params.K
+    D, F, E = x_perm.shape[-1], gate_scale.shape[-1], params.E
+    if x_perm.shape[0] < R or out_perm.shape[0] < R:
+        raise ValueError("x_perm and out_perm need T * K rows")
+    _dense("x_perm", x_perm, (x_perm.shape[0], D), torch.int8)
+    _dense("x_scale", x_scale, (x_scale.shape[0],), torch.float32)
+    if x_scale.shape[0] < (R if row_pair is None else params.T):
+        raise ValueError("x_scale is too short")
+    if row_pair is not None:
+        _dense("row_pair", row_pair, (row_pair.shape[0],), torch.int32)
+        if row_pair.shape[0] < R:
+            raise ValueError("row_pair is too short")
+    for what, t, n in (("gate_scale", gate_scale, F), ("up_scale", up_scale, F),
+                       ("down_scale", down_scale, D)):
+        _dense(what, t, (E, n), torch.float32)
+    _dense("w_gate_up", w_gate_up, (E, 2 * F * D), torch.int8)
+    _dense("w_down", w_down, (E, D * F), torch.int8)
+    _dense("out_perm", out_perm, (out_perm.shape[0], D), torch.bfloat16)
+    _check(lib().llep_grouped_ffn_int8(
+        ctypes.byref(params), ctypes.byref(bufs.struct), device, _ptr(x_perm), _ptr(x_scale),
+        _ptr(row_pair), _ptr(w_gate_up), _ptr(gate_scale), _ptr(up_scale), _ptr(w_down),
+        _ptr(down_scale), D, F, _ptr(out_perm), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "llep_grouped_ffn_int8")

@@ -567,4 +567,134 @@ int llep_clip_gradients(int32_t n, const llep_gradient *grads, float max_norm, f
   return hip_result(llep::launch_clip(a, stream), "llep_clip_gradients");
 }
 
+int32_t llep_int8_row_bytes(int32_t D) {
+  if (D < 1 || D > LLEP_MAX_FFN_DIM) return -1;
+  return (D + 63) / 64 * 64;
+}
+
+int llep_quantize_rows(int64_t R, int32_t D, llep_dtype dtype, const void *x, int8_t *q,
+                       int32_t q_bytes, float *scale, hipStream_t stream) {
+  const size_t eb = elem_bytes(dtype);
+  if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  if (R < 0) return fail(LLEP_E_ARG, "R < 0");
+  if (D < 1 || D > LLEP_MAX_FFN_DIM) return fail(LLEP_E_ARG, "D outside [1, LLEP_MAX_FFN_DIM]");
+  if (q_bytes < D || q_bytes % 64 != 0)
+    return fail(LLEP_E_ARG, "q_bytes must be a multiple of 64, at least D");
+  if (R > 0 && (!x || !q || !scale)) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned_to(x, eb) || !aligned16(q) || !aligned_to(scale, 4))
+    return fail(LLEP_E_ARG, "x, q or scale not aligned");
+  return hip_result(llep::launch_quantize_rows(R, D, dtype, x, q, q_bytes, scale, stream),
+                    "llep_quantize_rows");
+}
+
+size_t llep_packed_int8_bytes(int32_t E, int32_t N, int32_t K) {
+  if (E < 1 || E > LLEP_MAX_EXPERTS || N < 1 || N > LLEP_MAX_INT8_COLUMNS || K < 1 ||
+      K > LLEP_MAX_FFN_DIM)
+    return 0;
+  return size_t(E) * ((size_t(N) + 15) / 16 * 16) * ((size_t(K) + 63) / 64 * 64);
+}
+
+int llep_pack_int8(int32_t E, int32_t N, int32_t K, const int8_t *w, const int8_t *w_up,
+                   int8_t *packed, hipStream_t stream) {
+  if (llep_packed_int8_bytes(E, N, K) == 0)
+    return fail(LLEP_E_ARG, "E, N or K outside its range");
+  if (w_up && (N % 32 != 0 || N > LLEP_MAX_FFN_DIM))
+    return fail(LLEP_E_ARG, "gate and up rows: N must be a multiple of 32, at most LLEP_MAX_FFN_DIM");
+  if (!w || !packed) return fail(LLEP_E_ARG, "a weight pointer is null");
+  if (!aligned16(packed)) return fail(LLEP_E_ARG, "packed weights not 16-byte aligned");
+  return hip_result(llep::launch_pack_int8(E, N, K, w, w_up, packed, stream), "llep_pack_int8");
+}
+
+size_t llep_int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+  if (M < 0 || M > LLEP_MAX_INT8_ROWS || llep_packed_int8_bytes(1, N, K) == 0) return 0;
+  return llep::int8_matmul_workspace_bytes(M, N, K);
+}
+
+int llep_int8_matmul(int64_t M, int32_t N, int32_t K, const int8_t *x, int32_t x_bytes,
+                     const float *x_scale, const int8_t *w_packed, const float *w_scale,
+                     llep_dtype dtype, void *out, void *workspace, size_t workspace_bytes,
+                     hipStream_t stream) {
+  const size_t eb = elem_bytes(dtype);
+  if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  if (M < 0 || M > LLEP_MAX_INT8_ROWS) return fail(LLEP_E_ARG, "M outside [0, LLEP_MAX_INT8_ROWS]");
+  if (llep_packed_int8_bytes(1, N, K) == 0) return fail(LLEP_E_ARG, "N or K outside its range");
+  if (x_bytes % 64 != 0 || x_bytes < llep_int8_row_bytes(K) || x_bytes > LLEP_MAX_FFN_DIM)
+    return fail(LLEP_E_ARG, "x_bytes must be a multiple of 64 from llep_int8_row_bytes(K) on");
+  if (!w_packed || !w_scale || (M > 0 && (!x || !x_scale || !out)))
+    return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned16(x) || !aligned16(w_packed) || !aligned16(w_scale) || !aligned16(out) ||
+      !aligned_to(x_scale, 4))
+    return fail(LLEP_E_ARG, "data not 16-byte aligned");
+  const size_t need = llep::int8_matmul_workspace_bytes(M, N, K);
+  if (workspace_bytes < need || (need > 0 && !workspace))
+    return fail(LLEP_E_WORKSPACE,
+                "workspace missing or smaller than llep_int8_matmul_workspace_bytes");
+  if (!aligned_to(workspace, 256)) return fail(LLEP_E_WORKSPACE, "workspace not 256-byte aligned");
+  llep::Int8MatmulArgs a = {};
+  a.M = M;
+  a.N = N;
+  a.K = K;
+  a.x_bytes = x_bytes;
+  a.dtype = dtype;
+  a.x = x;
+  a.w = w_packed;
+  a.x_scale = x_scale;
+  a.w_scale = w_scale;
+  a.out = out;
+  a.ws = workspace;
+  return hip_result(llep::launch_int8_matmul(a, stream), "llep_int8_matmul");
+}
+
+size_t llep_grouped_ffn_int8_workspace_bytes(const llep_plan_params *params, int32_t F) {
+  if (check_params(params) != LLEP_OK || F < 1 || F > LLEP_MAX_FFN_DIM) return 0;
+  return llep::ffn_int8_workspace_bytes(params->T * params->K, params->E, params->P, F);
+}
+
+int llep_grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buffers *plan,
+                          int32_t device, const int8_t *x_perm, const float *x_scale,
+                          const int32_t *row_pair, const int8_t *w_gate_up_packed,
+                          const float *gate_scale, const float *up_scale,
+                          const int8_t *w_down_packed, const float *down_scale, int32_t D,
+                          int32_t F, void *out_perm, void *workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  int rc = check_params(params);
+  if (rc != LLEP_OK) return rc;
+  if ((rc = check_plan_buffers(plan)) != LLEP_OK) return rc;
+  if ((rc = check_ffn_dims(D, F, LLEP_BF16)) != LLEP_OK) return rc;
+  if (device < -1 || device >= params->P) return fail(LLEP_E_ARG, "device outside [-1, P)");
+  if (!x_perm || !x_scale || !w_gate_up_packed || !gate_scale || !up_scale || !w_down_packed ||
+      !down_scale || !out_perm)
+    return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned16(x_perm) || !aligned16(w_gate_up_packed) || !aligned16(w_down_packed) ||
+      !aligned16(gate_scale) || !aligned16(up_scale) || !aligned16(down_scale) ||
+      !aligned16(out_perm) || !aligned_to(x_scale, 4) || !aligned_to(row_pair, 4))
+    return fail(LLEP_E_ARG, "data not 16-byte aligned");
+  const size_t need = llep_grouped_ffn_int8_workspace_bytes(params, F);
+  if (!workspace || workspace_bytes < need)
+    return fail(LLEP_E_WORKSPACE,
+                "workspace missing or smaller than llep_grouped_ffn_int8_workspace_bytes");
+  if (!aligned_to(workspace, 256)) return fail(LLEP_E_WORKSPACE, "workspace not 256-byte aligned");
+  llep::FfnInt8Args a = {};
+  a.R = params->T * params->K;
+  a.P = params->P;
+  a.E = params->E;
+  a.D = D;
+  a.F = F;
+  a.K = params->K;
+  a.device = device;
+  a.groups = plan->groups;
+  a.group_begin = plan->group_begin;
+  a.row_pair = row_pair;
+  a.x_perm = x_perm;
+  a.w_gate_up = w_gate_up_packed;
+  a.w_down = w_down_packed;
+  a.x_scale = x_scale;
+  a.gate_scale = gate_scale;
+  a.up_scale = up_scale;
+  a.down_scale = down_scale;
+  a.out_perm = out_perm;
+  a.ws = workspace;
+  return hip_result(llep::launch_ffn_int8(a, stream), "llep_grouped_ffn_int8");
+}
+
 }  // extern "C"

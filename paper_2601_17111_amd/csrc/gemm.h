@@ -54,8 +54,15 @@ constexpr int kGroupM = LLEP_GROUP_M;  // m-tiles per super-row of the tile orde
 // Epilogues: plain bf16 C (the forward's down projection, the backward's g, u
 // and input gradient), SwiGLU of gate/up column pairs (a training forward also
 // stores the gate / up values), and the SwiGLU backward (C = d act; reads the
-// gate / up values, writes their gradients and the activation).
-enum Epilogue : int { kEpiPlain = 0, kEpiSwiglu = 1, kEpiSwigluBwd = 2 };
+// gate / up values, writes their gradients and the activation). The last two
+// are of the 8-bit GEMMs (int8.hip).
+enum Epilogue : int {
+  kEpiPlain = 0,
+  kEpiSwiglu = 1,
+  kEpiSwigluBwd = 2,
+  kEpiInt8 = 3,
+  kEpiInt8Swiglu = 4
+};
 
 struct GemmArgs {
   const uint16_t *A;
@@ -81,6 +88,63 @@ struct GemmArgs {
   uint16_t *act;
 };
 
+// 8-bit GEMMs (kEpiInt8, kEpiInt8Swiglu): operands of signed bytes. A byte
+// matrix is handled as one of half as many 2-byte elements: A, lda, B,
+// b_expert_stride and Kdim above count pairs of bytes, and a 32-deep slice
+// holds 64 bytes of k, which the matrix cores take in two steps of 32.
+struct Int8GemmArgs : GemmArgs {
+  const float *a_scale;       // per token (row_pair: of row r, token row_pair[r] / K) or per row
+  const int32_t *row_pair;    // or null
+  int32_t K;
+  const float *b_scale, *b_scale2;  // per expert and column; SwiGLU: of gate and of up columns
+  int64_t scale_stride;       // between experts' b_scale
+  int64_t M;                  // dense: rows of A
+  bool f32_out;               // kEpiInt8: C is float32, else bfloat16
+};
+
+// The value that the sum `acc` of an 8-bit product stands for, in every 8-bit
+// kernel the same expression.
+__device__ __forceinline__ float int8_value(int32_t acc, float a_scale, float b_scale) {
+  return float(acc) * a_scale * b_scale;
+}
+__device__ __forceinline__ float int8_swiglu(float g, float u) {
+  return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
+}
+__device__ __forceinline__ float int8_row_scale(const Int8GemmArgs &g, int64_t row) {
+  return g.a_scale[g.row_pair ? int64_t(g.row_pair[row] / g.K) : row];
+}
+// four consecutive scales from column c on; columns from N on: 0
+__device__ __forceinline__ f32x4 int8_col_scales(const float *s, int c, int N) {
+  if ((N & 3) == 0) {
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    return c < N ? *reinterpret_cast<const f32x4 *>(s + c) : zero;
+  }
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = c + i < N ? s[c + i] : 0.0f;
+  return v;
+}
+// four consecutive values of a row of C from column c on, those below N
+template <typename Out>
+__device__ __forceinline__ void int8_store4(Out *row, int c, int N, const f32x4 v) {
+  if ((N & 3) == 0) {
+    if (c >= N) return;
+    if constexpr (sizeof(Out) == 4)
+      *reinterpret_cast<f32x4 *>(row + c) = v;
+    else
+      *reinterpret_cast<uint2 *>(row + c) =
+          make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < N) {
+      if constexpr (sizeof(Out) == 4)
+        row[c + i] = v[i];
+      else
+        row[c + i] = f32_to_bf16(v[i]);
+    }
+}
 
 // ---------------------------------------------------------------------------
 // bf16 MFMA grouped GEMM, 256 x BN tiles, eight waves of WM x WN.
@@ -284,14 +348,16 @@ struct LaunchSched {
 // of whose slices has been requested yet), through the LDS ring at `smem`
 // (ring_bytes<BN>() bytes, 1 KB aligned).
 template <int BN, int WAVES_M, int WAVES_N, int kEpi, bool kABlocked, bool kCBlocked,
-          class Sched>
-__device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoord t,
-                                           Sched &sched) {
+          class Sched, class Args>
+__device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t, Sched &sched) {
   constexpr int BM = 256;
   constexpr int NW = WAVES_M * WAVES_N;
   constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N;
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr bool kSwiglu = kEpi == kEpiSwiglu;
+  constexpr bool kInt8 = kEpi == kEpiInt8 || kEpi == kEpiInt8Swiglu;
+  using Frag = std::conditional_t<kInt8, i32x4, bf16x8>;  // 16 bytes of a row along k
+  using Acc = std::conditional_t<kInt8, i32x16, f32x16>;
   // DMA blocks (16 rows each) per stage, dealt round-robin over the waves:
   // every wave has A_PER_WAVE A blocks and B_FULL B blocks, the first B_REM
   // waves one B block more. Waits count the PER_STAGE instructions every
@@ -309,7 +375,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
   static_assert(A_BLOCKS % NWD == 0 && PER_STAGE > 0 && NWD <= NW, "DMA split");
   static_assert(WM % 32 == 0 && WN % 32 == 0, "wave tile");
   static_assert(kAhead == 4, "waits below are written for four slices ahead");
-  static_assert(!kSwiglu || (WN % 64) == 0, "SwiGLU needs gate/up column pairs per wave");
+  static_assert((!kSwiglu && kEpi != kEpiInt8Swiglu) || (WN % 64) == 0, "SwiGLU needs gate/up column pairs per wave");
   // stage s: A rows at s * STAGE_BYTES, then B rows; the last two stages are
   // also the epilogue's staging area
   constexpr uint32_t STAGE_BYTES = A_STAGE_BYTES + B_STAGE_BYTES;
@@ -397,23 +463,29 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
   // read from LDS while the current one feeds the MFMAs, so LDS latency hides
   // behind the MFMAs.
   static_assert(kSK == 32, "two k-steps per slice");
-  auto read_frags = [&](int st, int ks, bf16x8 (&fa)[TM], bf16x8 (&fb)[TN]) {
+  auto mfma = [](const Frag &b, const Frag &a, const Acc &c) {
+    if constexpr (kInt8)
+      return __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+  };
+  auto read_frags = [&](int st, int ks, Frag (&fa)[TM], Frag (&fb)[TN]) {
     const uint16_t *a_s = stageA(st);
     const uint16_t *b_s = stageB(st);
     const int kc = ks * 2 + (lane >> 5);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
-      fa[i] = *reinterpret_cast<const bf16x8 *>(&a_s[lds_swz32(wm * WM + i * 32 + (lane & 31), kc)]);
+      fa[i] = *reinterpret_cast<const Frag *>(&a_s[lds_swz32(wm * WM + i * 32 + (lane & 31), kc)]);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-      fb[j] = *reinterpret_cast<const bf16x8 *>(&b_s[lds_swz32(wn * WN + j * 32 + (lane & 31), kc)]);
+      fb[j] = *reinterpret_cast<const Frag *>(&b_s[lds_swz32(wn * WN + j * 32 + (lane & 31), kc)]);
   };
-  auto mfma_step = [&](f32x16 (&acc)[TM][TN], const bf16x8 (&fa)[TM], const bf16x8 (&fb)[TN]) {
+  auto mfma_step = [&](Acc (&acc)[TM][TN], const Frag (&fa)[TM], const Frag (&fb)[TN]) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
   };
   auto next_stage = [](int st) { return st + 1 == kStages ? 0 : st + 1; };
 
@@ -431,15 +503,15 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
   // dma_wave: std::true_type for the waves that issue the DMA, else
   // std::false_type (their DMA side operations are empty)
   auto side_op = [&](auto dma_wave, int q, int dma_lo, int st_next, int ks_next,
-                     bf16x8 (&fa)[TM], bf16x8 (&fb)[TN], int st_dma, int kt_dma) {
+                     Frag (&fa)[TM], Frag (&fb)[TN], int st_dma, int kt_dma) {
     constexpr bool kDmaWave = decltype(dma_wave)::value;
     if (q < TM) {
       const uint16_t *a_s = stageA(st_next);
-      fa[q] = *reinterpret_cast<const bf16x8 *>(
+      fa[q] = *reinterpret_cast<const Frag *>(
           &a_s[lds_swz32(wm * WM + q * 32 + (lane & 31), ks_next * 2 + (lane >> 5))]);
     } else if (q < NR) {
       const uint16_t *b_s = stageB(st_next);
-      fb[q - TM] = *reinterpret_cast<const bf16x8 *>(
+      fb[q - TM] = *reinterpret_cast<const Frag *>(
           &b_s[lds_swz32(wn * WN + (q - TM) * 32 + (lane & 31), ks_next * 2 + (lane >> 5))]);
     } else if constexpr (kDmaWave) {
       const int d = dma_lo + q - NR;
@@ -454,15 +526,14 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
         dma16(Bb + kbb, offB[B_SLOTS - 1], b_st + (wave + NWD * B_FULL) * 1024);
     }
   };
-  auto interleaved_step = [&](auto dma_wave, f32x16 (&acc)[TM][TN], const bf16x8 (&fa)[TM],
-                              const bf16x8 (&fb)[TN], bf16x8 (&fa_next)[TM],
-                              bf16x8 (&fb_next)[TN], int st_next, int ks_next, int dma_lo,
+  auto interleaved_step = [&](auto dma_wave, Acc (&acc)[TM][TN], const Frag (&fa)[TM],
+                              const Frag (&fb)[TN], Frag (&fa_next)[TM],
+                              Frag (&fb_next)[TN], int st_next, int ks_next, int dma_lo,
                               int dma_hi, int st_dma, int kt_dma) {
     const int NS = NR + (dma_hi - dma_lo);
 #pragma unroll
     for (int s = 0; s < NM; ++s) {
-      acc[s / TN][s % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          fb[s % TN], fa[s / TN], acc[s / TN][s % TN], 0, 0, 0);
+      acc[s / TN][s % TN] = mfma(fb[s % TN], fa[s / TN], acc[s / TN][s % TN]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < NR + ND; ++q) {
@@ -479,13 +550,13 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
     // ask for the tile after this one (read after the barrier that ends the
     // loop; rewritten only after the barrier that ends the epilogue)
     sched.request();
-    f32x16 acc[TM][TN];
+    Acc acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+        for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
     // A wave whose 32 x 32 blocks all lie past the tile's last valid row or
     // column (a group's last, partly filled m-tile; the last n-tile) has no
     // MFMA work: it runs the same slice loop with the same DMA requests and
@@ -496,7 +567,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
     const int active =
         __builtin_amdgcn_readfirstlane(int(t.rows_valid > wm * WM && t.cols_valid > wn * WN));
     if (active) {
-      bf16x8 fa0[TM], fb0[TN], fa1[TM], fb1[TN];
+      Frag fa0[TM], fb0[TN], fa1[TM], fb1[TN];
       // slice kt sits in stage kt % kStages; st tracks the slice being read,
       // st_req the stage of slice kt + kAhead
       int st = 0, st_req = kAhead % kStages, kt_req = kAhead;
@@ -799,6 +870,88 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs g, char *smem, TileCoo
           for (int gq = 0; gq < 4; ++gq) {
             gcur[gq] = gnxt[gq];
             ucur[gq] = unxt[gq];
+          }
+        }
+      }
+    } else if constexpr (kEpi == kEpiInt8Swiglu) {
+      // float32 activations, row-major by row of A: 32 rows x 32 columns at a
+      // time through the staging area, out as whole 128-byte row pieces
+      constexpr int RS = 128 + 16;
+      static_assert(32 * RS <= STAGING, "staging");
+      const int F = g.N / 2;
+      float *act = reinterpret_cast<float *>(g.C);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i * 32 >= rows_w) break;
+        const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
+        const float sa = int8_row_scale(g, row0 + min(lane & 31, rows_w - i * 32 - 1));
+#pragma unroll
+        for (int p = 0; p < TN / 2; ++p) {
+          const int f = (c.n0 + wn * WN + p * 64) >> 1;
+          if (f >= F) continue;
+#pragma unroll
+          for (int gq = 0; gq < 4; ++gq) {
+            const int col = f + 8 * gq + 4 * h;
+            const f32x4 sg = int8_col_scales(g.b_scale + c.e * g.scale_stride, col, F);
+            const f32x4 su = int8_col_scales(g.b_scale2 + c.e * g.scale_stride, col, F);
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = int8_swiglu(int8_value(acc[i][2 * p][4 * gq + e], sa, sg[e]),
+                                 int8_value(acc[i][2 * p + 1][4 * gq + e], sa, su[e]));
+            *reinterpret_cast<f32x4 *>(stg + (lane & 31) * RS + (8 * gq + 4 * h) * 4) = v;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int row = 8 * q + (lane >> 3);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(stg + row * RS + (lane & 7) * 16);
+            if (i * 32 + row < rows_w)
+              *reinterpret_cast<f32x4 *>(act + (row0 + row) * F + f + (lane & 7) * 4) = v;
+          }
+        }
+      }
+    } else if constexpr (kEpi == kEpiInt8) {
+      static_assert(!kCBlocked, "row-major C");
+      // bfloat16 rows of whole 16-byte vectors go through the staging area as
+      // below; other C (float32, any N) are stored from the registers
+      constexpr int RS = WN * 2 + 16;
+      constexpr int CH = WN / 8;
+      static_assert(32 * RS <= STAGING, "staging");
+      const int ncol0 = c.n0 + wn * WN;
+      const bool staged = !g.f32_out && (g.N & 7) == 0;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i * 32 >= rows_w) break;
+        const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
+        const bool row_ok = i * 32 + (lane & 31) < rows_w;
+        const int64_t row = row0 + min(lane & 31, rows_w - i * 32 - 1);
+        const float sa = int8_row_scale(g, row);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int gq = 0; gq < 4; ++gq) {
+            const int col = ncol0 + j * 32 + 8 * gq + 4 * h;
+            const f32x4 sb = int8_col_scales(g.b_scale + c.e * g.scale_stride, col, g.N);
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = int8_value(acc[i][j][4 * gq + e], sa, sb[e]);
+            if (staged)
+              *reinterpret_cast<uint2 *>(stg + (lane & 31) * RS + (j * 32 + 8 * gq + 4 * h) * 2) =
+                  make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+            else if (row_ok && g.f32_out)
+              int8_store4(reinterpret_cast<float *>(g.C) + row * g.ldc, col, g.N, v);
+            else if (row_ok)
+              int8_store4(g.C + row * g.ldc, col, g.N, v);
+          }
+        if (staged) {
+          char *crow = reinterpret_cast<char *>(g.C + row0 * g.ldc + ncol0);
+#pragma unroll
+          for (int r0 = 0; r0 < 32 * CH; r0 += kWave) {
+            const int q = r0 + lane;
+            const int r = q / CH, ch = q % CH;
+            if (q < 32 * CH && i * 32 + r < rows_w && ncol0 + ch * 8 < g.N)
+              *reinterpret_cast<i32x4 *>(crow + int64_t(r) * g.ldc * 2 + ch * 16) =
+                  *reinterpret_cast<const i32x4 *>(stg + r * RS + ch * 16);
           }
         }
       }

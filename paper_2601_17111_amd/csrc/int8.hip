@@ -1,0 +1,529 @@
+// Products of 8-bit integers with a scale per token and per channel
+// (llep_quantize_rows, llep_int8_matmul, llep_grouped_ffn_int8):
+//   C[m][n] = s_a[m] s_b[n] sum_k A[m][k] B[n][k],
+// the sum exact in 32-bit integers, so that a result does not depend on which
+// kernel ran or how k was split.
+//
+// Weights are packed (llep_pack_int8) in blocks of 16 rows x 64 k, 1 KB each:
+// a matrix-core operand of 16 rows is one contiguous block. Two kernels:
+//   - tiles (gemm.h): 256 x 256 or 256 x 192 outputs per workgroup, operands
+//     through a ring in LDS, bound by the matrix cores;
+//   - stream (below): every wavefront reads its operands from memory straight
+//     into registers and the wavefronts of a workgroup split k, for few rows,
+//     where reading the weights once is the work.
+#include <algorithm>
+
+#include "gemm.h"
+#include "rows.h"
+
+namespace llep {
+
+// ---------------------------------------------------------------------------
+// 8-bit rows
+// ---------------------------------------------------------------------------
+
+struct QuantArgs {
+  int64_t R;
+  int32_t D, q_bytes;
+  const void *x;
+  int8_t *q;
+  float *scale;
+  // grouped: the rows of `device`'s groups (or of all), R of them at most
+  const int32_t *groups, *group_begin;
+  int32_t device, P;
+};
+
+template <typename T, int kThreads, int kVec, int kPer>
+__global__ __launch_bounds__(kThreads < kRowWg ? kRowWg : kThreads) void quantize_rows_kernel(
+    QuantArgs a) {
+  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
+  __shared__ float lds[RowReduce<kThreads>::kLds];
+  RowReduce<kThreads> red(lds);
+  const int t = threadIdx.x % kThreads;
+  const uint32_t D = a.D;
+  int64_t r0 = 0, r1 = a.R;
+  if (a.groups) {
+    const int lo = a.device < 0 ? a.group_begin[0] : a.group_begin[a.device];
+    const int hi = a.device < 0 ? a.group_begin[a.P] : a.group_begin[a.device + 1];
+    r0 = lo < hi ? a.groups[4 * lo + 2] : 0;
+    r1 = lo < hi ? a.groups[4 * (hi - 1) + 2] + a.groups[4 * (hi - 1) + 3] : 0;
+  }
+  const int first = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  for (int64_t row = r0 + int64_t(blockIdx.x) * kRows + first; row < r1;
+       row += int64_t(gridDim.x) * kRows) {
+    const T *x = static_cast<const T *>(a.x) + row * D;
+    float v[kPer][kVec];
+    float most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const uint32_t c = (j * kThreads + t) * kVec;
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[j][i] = 0.0f;
+      if (c < D) load_vec<T, kVec>(x + c, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(fabsf(v[j][i]))));
+    const RowScale s = row_scale(red.max_bits(most));
+    store_int8_row<kThreads, kVec, kPer>(a.q + row * a.q_bytes, D, a.q_bytes, t, v, s);
+    if (t == 0) a.scale[row] = s.scale;
+  }
+}
+
+// Odd rows too long for the registers: read once for the maximum, again from
+// the cache for the values.
+template <typename T>
+__global__ __launch_bounds__(1024) void quantize_long_rows_kernel(QuantArgs a) {
+  __shared__ float lds[RowReduce<1024>::kLds];
+  RowReduce<1024> red(lds);
+  for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
+    const T *x = static_cast<const T *>(a.x) + row * a.D;
+    float most = 0.0f;
+    for (int c = threadIdx.x; c < a.D; c += 1024) {
+      float v[1];
+      load_vec<T, 1>(x + c, v);
+      most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(fabsf(v[0]))));
+    }
+    const RowScale s = row_scale(red.max_bits(most));
+    int8_t *q = a.q + row * a.q_bytes;
+    for (int c = threadIdx.x; c < a.q_bytes; c += 1024) {
+      float v[1] = {0.0f};
+      if (c < a.D) load_vec<T, 1>(x + c, v);
+      q[c] = c < a.D ? int8_t(quantize(v[0], s)) : int8_t(0);
+    }
+    if (threadIdx.x == 0) a.scale[row] = s.scale;
+  }
+}
+
+template <typename T, int kThreads, int kVec, int kPer>
+hipError_t run_quantize(const QuantArgs &a, hipStream_t stream) {
+  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
+  const int64_t grid = std::min<int64_t>((a.R + kRows - 1) / kRows, 65536);
+  hipLaunchKernelGGL((quantize_rows_kernel<T, kThreads, kVec, kPer>), dim3(uint32_t(grid)),
+                     dim3(kRows * kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
+  const int32_t D = a.D;
+  if (a.R == 0) return hipSuccess;
+  if (D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0) {
+    if (D <= 2048) return run_quantize<T, 256, 8, 1>(a, stream);
+    if (D <= 4096) return run_quantize<T, 256, 8, 2>(a, stream);
+    if (D <= 8192) return run_quantize<T, 256, 8, 4>(a, stream);
+    return run_quantize<T, 1024, 8, 8>(a, stream);
+  }
+  if (D <= 1024) return run_quantize<T, 256, 1, 4>(a, stream);
+  if (D <= 8192) return run_quantize<T, 1024, 1, 8>(a, stream);
+  // (a range of groups has rows of whole vectors: F % 64 == 0)
+  hipLaunchKernelGGL(quantize_long_rows_kernel<T>, dim3(uint32_t(std::min<int64_t>(a.R, 65536))),
+                     dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_rows(int64_t R, int32_t D, llep_dtype dtype, const void *x, int8_t *q,
+                                int32_t q_bytes, float *scale, hipStream_t stream) {
+  QuantArgs a = {};
+  a.R = R;
+  a.D = D;
+  a.q_bytes = q_bytes;
+  a.x = x;
+  a.q = q;
+  a.scale = scale;
+  return dtype == LLEP_BF16 ? quantize_t<uint16_t>(a, stream) : quantize_t<float>(a, stream);
+}
+
+// ---------------------------------------------------------------------------
+// packing: 16 bytes of a packed row per thread
+// ---------------------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void pack_int8_kernel(const int8_t *__restrict__ w0,
+                                                        const int8_t *__restrict__ w1, int64_t E,
+                                                        int32_t N, int32_t K, int32_t Np,
+                                                        int32_t Kp, int8_t *__restrict__ out) {
+  const int64_t chunks = E * (int64_t(Np) * Kp / 16);
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < chunks;
+       i += int64_t(gridDim.x) * 256) {
+    const int64_t blk = i >> 6;
+    const int kbs = Kp / 64;
+    const int kb = int(blk % kbs), nb = int(blk / kbs % (Np / 16));
+    const int64_t e = blk / kbs / (Np / 16);
+    int n = nb * 16 + (int(i) >> 2 & 15);
+    const int k = kb * 64 + (int(i) & 3) * 16;
+    // two matrices: 32 rows of the first, then the matching 32 of the second
+    const int8_t *src = w0;
+    bool ok = n < N;
+    if (w1) {
+      src = n & 32 ? w1 : w0;
+      n = (n >> 6) * 32 + (n & 31);
+      ok = n < N;
+    }
+    uint32_t v[4] = {0u, 0u, 0u, 0u};
+    if (ok) {
+      const int8_t *p = src + (e * N + n) * K + k;
+      if (K % 16 == 0 && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+        if (k < K) {
+          const uint4 q = *reinterpret_cast<const uint4 *>(p);
+          v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < 16; ++b)
+          if (k + b < K) v[b / 4] |= (uint32_t(p[b]) & 255u) << (8 * (b % 4));
+      }
+    }
+    reinterpret_cast<uint4 *>(out)[i] = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+hipError_t launch_pack_int8(int32_t E, int32_t N, int32_t K, const int8_t *w0, const int8_t *w1,
+                            int8_t *out, hipStream_t stream) {
+  const int32_t Np = w1 ? 2 * N : (N + 15) / 16 * 16, Kp = (K + 63) / 64 * 64;
+  const int64_t blocks = (E * (int64_t(Np) * Kp / 16) + 255) / 256;
+  hipLaunchKernelGGL(pack_int8_kernel, dim3(uint32_t(std::min<int64_t>(blocks, 65536))), dim3(256),
+                     0, stream, w0, w1, int64_t(E), N, K, Np, Kp, out);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// stream: few rows
+//
+// An item is up to 16 kMB rows of one group (of A, dense) by 16 kNB packed
+// rows of the weights; a workgroup of kWaves wavefronts takes one item at a
+// time, each wavefront a part of k, and adds the parts up through LDS.
+// v_mfma_i32_16x16x64_i8 takes a 1 KB block of the weights as its first
+// operand (lane l: row l % 16, bytes 16 (l / 16) .. + 15 of its 64), 16 rows of
+// A likewise as its second; lane l then holds, of row l % 16 of A, the columns
+// 4 (l / 16) .. + 3.
+// ---------------------------------------------------------------------------
+
+template <int kMB, int kNB, int kWaves, bool kGrouped, bool kSwigluOut>
+__global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArgs g) {
+  constexpr int kUnroll = kMB * kNB >= 8 ? 2 : 4;  // blocks of k requested together
+  __shared__ i32x4 part[kWaves][kMB * kNB][kWave];
+  static_assert(!kSwigluOut || kNB == 4, "32 gate rows and the matching 32 up rows");
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int nkb = g.Kdim / 32;               // blocks of 64 k
+  const int n_blk = (g.N + 15) / 16;         // blocks of 16 packed rows
+  const int n_unit = (n_blk + kNB - 1) / kNB;
+  const int n_mt = kGrouped ? *g.n_mtiles : int((g.M + 16 * kMB - 1) / (16 * kMB));
+  const int kb0 = nkb * wave / kWaves, kb1 = nkb * (wave + 1) / kWaves;
+  for (int64_t item = blockIdx.x; item < int64_t(n_mt) * n_unit; item += gridDim.x) {
+    const int mt = int(item / n_unit), unit = int(item % n_unit);
+    int e = 0;
+    int64_t row0 = int64_t(mt) * 16 * kMB;
+    int rows;
+    if (kGrouped) {
+      const int4 te = g.tiles[mt];
+      const int32_t *gr = g.groups + 4 * te.x;
+      e = gr[1];
+      row0 = int64_t(gr[2]) + te.y * 16 * kMB;
+      rows = min(16 * kMB, gr[3] - te.y * 16 * kMB);
+    } else {
+      rows = int(min<int64_t>(16 * kMB, g.M - row0));
+    }
+    const int8_t *A = reinterpret_cast<const int8_t *>(g.A) + row0 * g.lda * 2;
+    const int8_t *B = reinterpret_cast<const int8_t *>(g.B) + e * g.b_expert_stride * 2;
+    uint32_t offA[kMB], offB[kNB];
+#pragma unroll
+    for (int m = 0; m < kMB; ++m)
+      offA[m] = uint32_t(min(m * 16 + (lane & 15), rows - 1)) * uint32_t(g.lda * 2) + (lane >> 4) * 16;
+    const int8_t *Bu = B + int64_t(unit) * kNB * g.b_blk_stride;
+#pragma unroll
+    for (int n = 0; n < kNB; ++n)  // past the last block: the last one again, not stored
+      offB[n] = uint32_t(min(n, n_blk - 1 - unit * kNB)) * uint32_t(g.b_blk_stride) +
+                (lane & 15) * 64 + (lane >> 4) * 16;
+    i32x4 acc[kMB][kNB];
+#pragma unroll
+    for (int m = 0; m < kMB; ++m)
+#pragma unroll
+      for (int n = 0; n < kNB; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
+    auto steps = [&](auto count, int kb) {
+      constexpr int kU = decltype(count)::value;
+      i32x4 fa[kU][kMB], fb[kU][kNB];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+#pragma unroll
+        for (int n = 0; n < kNB; ++n)
+          fb[u][n] = *reinterpret_cast<const i32x4 *>(Bu + int64_t(kb + u) * 1024 + offB[n]);
+#pragma unroll
+        for (int m = 0; m < kMB; ++m)
+          fa[u][m] = *reinterpret_cast<const i32x4 *>(A + (kb + u) * 64 + offA[m]);
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int m = 0; m < kMB; ++m)
+#pragma unroll
+          for (int n = 0; n < kNB; ++n)
+            acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][n], fa[u][m], acc[m][n], 0, 0, 0);
+    };
+    int kb = kb0;
+    for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
+    for (; kb < kb1; ++kb) steps(std::integral_constant<int, 1>{}, kb);
+    if constexpr (kWaves > 1) {
+#pragma unroll
+      for (int m = 0; m < kMB; ++m)
+#pragma unroll
+        for (int n = 0; n < kNB; ++n) part[wave][m * kNB + n][lane] = acc[m][n];
+      __syncthreads();
+    }
+    // the sum over the wavefronts of a 16 x 16 block
+    auto total = [&](int m, int n) {
+      if constexpr (kWaves == 1) {
+        return acc[m][n];
+      } else {
+        i32x4 s = part[0][m * kNB + n][lane];
+        for (int w = 1; w < kWaves; ++w) s += part[w][m * kNB + n][lane];
+        return s;
+      }
+    };
+    if constexpr (kSwigluOut) {
+      const int F = g.N / 2;
+#pragma unroll
+      for (int q = 0; q < kMB * 2; ++q) {  // 16 rows x 16 activation columns
+        if (kWaves > 1 && q % kWaves != wave) continue;
+        const int m = q / 2, half = q % 2;
+        const i32x4 sg = total(m, half), su = total(m, 2 + half);
+        const int r = m * 16 + (lane & 15), col = unit * 32 + half * 16 + (lane >> 4) * 4;
+        if (r >= rows) continue;
+        const float sa = int8_row_scale(g, row0 + r);
+        const f32x4 cg = int8_col_scales(g.b_scale + e * g.scale_stride, col, F);
+        const f32x4 cu = int8_col_scales(g.b_scale2 + e * g.scale_stride, col, F);
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = int8_swiglu(int8_value(sg[i], sa, cg[i]), int8_value(su[i], sa, cu[i]));
+        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(g.C) + (row0 + r) * F + col) = v;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kMB * kNB; ++q) {
+        if (kWaves > 1 && q % kWaves != wave) continue;
+        const int m = q / kNB, n = q % kNB;
+        const i32x4 s = total(m, n);
+        const int r = m * 16 + (lane & 15), col = (unit * kNB + n) * 16 + (lane >> 4) * 4;
+        if (r >= rows || col >= g.N) continue;
+        const float sa = int8_row_scale(g, row0 + r);
+        const f32x4 cb = int8_col_scales(g.b_scale + e * g.scale_stride, col, g.N);
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = int8_value(s[i], sa, cb[i]);
+        if (g.f32_out)
+          int8_store4(reinterpret_cast<float *>(g.C) + (row0 + r) * g.ldc, col, g.N, v);
+        else
+          int8_store4(g.C + (row0 + r) * g.ldc, col, g.N, v);
+      }
+    }
+    if constexpr (kWaves > 1) __syncthreads();  // the parts are read before the next item's
+  }
+}
+
+// ---------------------------------------------------------------------------
+// tiles
+// ---------------------------------------------------------------------------
+
+// Hand-out of a dense product's tiles: those of LaunchSched, computed from M.
+template <int BN>
+struct DenseSched {
+  static constexpr bool kOpaqueLane = false;
+  static constexpr bool kCoherentC = false;
+  int64_t M;
+  int N, nk, n_mt, n_nt, G, slot, it;
+  __device__ __forceinline__ explicit DenseSched(const Int8GemmArgs &g) {
+    M = g.M;
+    N = g.N;
+    nk = g.Kdim / kSK;
+    n_mt = int((M + kTileM - 1) / kTileM);
+    n_nt = (N + BN - 1) / BN;
+    G = gridDim.x;
+    slot = (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8;
+    it = 0;
+  }
+  __device__ __forceinline__ bool tile(int64_t u, TileCoord &t) const {
+    if (u >= int64_t(n_mt) * n_nt) return false;
+    const int sr = int(u / (int64_t(kGroupM) * n_nt));
+    const int rem = int(u - int64_t(sr) * kGroupM * n_nt);
+    const int gm = min(kGroupM, n_mt - sr * kGroupM);
+    t.e = 0;
+    t.row0 = 0;
+    t.prow0 = 0;
+    t.mt = sr * kGroupM + rem % gm;
+    t.m0 = t.mt * kTileM;
+    t.rows_valid = int(min<int64_t>(kTileM, M - t.m0));
+    t.n0 = rem / gm * BN;
+    t.cols_valid = min(BN, N - t.n0);
+    t.nk = nk;
+    return true;
+  }
+  __device__ __forceinline__ bool first(TileCoord &t) const { return tile(slot, t); }
+  __device__ __forceinline__ void request() {}
+  __device__ __forceinline__ bool next(TileCoord &t) { return tile(int64_t(++it) * G + slot, t); }
+  __device__ __forceinline__ void done(const TileCoord &, bool) {}
+};
+
+template <int BN, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N)
+__attribute__((amdgpu_waves_per_eu(WAVES_M * WAVES_N / 4, WAVES_M * WAVES_N / 4)))
+void int8_tiles_kernel(Int8GemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes<BN>()];
+  std::conditional_t<kGrouped, LaunchSched<256, BN>, DenseSched<BN>> sched(g);
+  TileCoord t;
+  if (!sched.first(t)) return;
+  gemm_tiles<BN, WAVES_M, WAVES_N, kEpi, false, false>(g, smem, t, sched);
+}
+
+// ---------------------------------------------------------------------------
+// launch
+// ---------------------------------------------------------------------------
+
+// Rows up to which a product takes the stream: 64 per item read the weights
+// once; beyond, tiles do more work per byte.
+constexpr int64_t kInt8StreamRows = 64;
+
+template <bool kGrouped, bool kSwigluOut>
+hipError_t launch_int8_stream(const Int8GemmArgs &g, int64_t rows, int64_t items_most,
+                              hipStream_t stream) {
+  const int grid = int(std::min<int64_t>(items_most, 16384));
+  if (rows <= 16)
+    hipLaunchKernelGGL((int8_stream_kernel<1, 4, 4, kGrouped, kSwigluOut>), dim3(grid), dim3(256), 0,
+                       stream, g);
+  else
+    hipLaunchKernelGGL((int8_stream_kernel<4, 4, 4, kGrouped, kSwigluOut>), dim3(grid), dim3(256), 0,
+                       stream, g);
+  return hipGetLastError();
+}
+
+size_t int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+  return 0;
+}
+
+hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream) {
+  if (a.M == 0) return hipSuccess;
+  Int8GemmArgs g = {};
+  const int32_t Kp = (a.K + 63) / 64 * 64;
+  g.A = reinterpret_cast<const uint16_t *>(a.x);
+  g.lda = a.x_bytes / 2;
+  g.B = reinterpret_cast<const uint16_t *>(a.w);
+  g.b_blk_stride = int64_t(Kp) * 16;
+  g.C = static_cast<uint16_t *>(a.out);
+  g.ldc = a.N;
+  g.N = a.N;
+  g.Kdim = Kp / 2;
+  g.a_scale = a.x_scale;
+  g.b_scale = a.w_scale;
+  g.M = a.M;
+  g.f32_out = a.dtype == LLEP_F32;
+  if (a.M <= kInt8StreamRows)
+    return launch_int8_stream<false, false>(g, a.M, (int64_t(a.N) + 63) / 64, stream);
+  const int grid = (cu_count() + 7) / 8 * 8;
+  hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8, false>), dim3(grid),
+                     dim3(64 * kWavesM * kWavesN), 0, stream, g);
+  return hipGetLastError();
+}
+
+// Workspace of the grouped FFN: the tile count (int at 0), the tile list, the
+// rows' activation scales, the activations in float32 and then in 8 bits.
+struct Int8Ws {
+  size_t tiles, scale, act, act_q, total;
+};
+static Int8Ws int8_ws(int64_t R, int32_t E, int32_t P, int32_t F) {
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  Int8Ws w;
+  w.tiles = 256;
+  // the shortest tiles have 16 rows
+  w.scale = w.tiles + up(size_t(R / 16 + 2 * int64_t(E) + P + 1) * 16);
+  w.act = w.scale + up(size_t(R) * 4);
+  w.act_q = w.act + up(size_t(R) * F * 4);
+  w.total = w.act_q + up(size_t(R) * F);
+  return w;
+}
+
+size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F) {
+  return int8_ws(R, E, P, F).total;
+}
+
+hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
+  if (a.R == 0) return hipSuccess;
+  const Int8Ws w = int8_ws(a.R, a.E, a.P, a.F);
+  char *ws = static_cast<char *>(a.ws);
+  int32_t *n_mtiles = reinterpret_cast<int32_t *>(ws);
+  int4 *tiles = reinterpret_cast<int4 *>(ws + w.tiles);
+  float *act = reinterpret_cast<float *>(ws + w.act);
+  int8_t *act_q = reinterpret_cast<int8_t *>(ws + w.act_q);
+  float *act_scale = reinterpret_cast<float *>(ws + w.scale);
+  // rows per expert on average (the routing is not known here)
+  const bool streams = a.R <= 24 * int64_t(a.E) && a.R <= 4096;
+  const int rows = !streams ? kTileM : a.R <= 4 * int64_t(a.E) ? 16 : 64;
+  hipError_t err = launch_tile_table(a.groups, a.group_begin, 2 * a.E + a.P, a.device, a.P, rows,
+                                     tiles, n_mtiles, stream);
+  if (err != hipSuccess) return err;
+  const int grid = (cu_count() + 7) / 8 * 8;
+  const int64_t mt_most = a.R / rows + std::min<int64_t>(a.R, 2 * int64_t(a.E) + a.P);
+  Int8GemmArgs g = {};
+  g.A = reinterpret_cast<const uint16_t *>(a.x_perm);
+  g.lda = a.D / 2;
+  g.B = reinterpret_cast<const uint16_t *>(a.w_gate_up);
+  g.b_expert_stride = int64_t(a.F) * a.D;
+  g.b_blk_stride = int64_t(a.D) * 16;
+  g.C = reinterpret_cast<uint16_t *>(act);
+  g.ldc = a.F;
+  g.groups = a.groups;
+  g.tiles = tiles;
+  g.n_mtiles = n_mtiles;
+  g.N = 2 * a.F;
+  g.Kdim = a.D / 2;
+  g.a_scale = a.x_scale;
+  g.row_pair = a.row_pair;
+  g.K = a.K;
+  g.b_scale = a.gate_scale;
+  g.b_scale2 = a.up_scale;
+  g.scale_stride = a.F;
+  if (streams) {
+    err = launch_int8_stream<true, true>(g, rows, mt_most * (a.F / 32), stream);
+  } else {
+    hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8Swiglu, true>), dim3(grid),
+                       dim3(64 * kWavesM * kWavesN), 0, stream, g);
+    err = hipGetLastError();
+  }
+  if (err != hipSuccess) return err;
+  QuantArgs q = {};
+  q.R = a.R;
+  q.D = q.q_bytes = a.F;
+  q.x = act;
+  q.q = act_q;
+  q.scale = act_scale;
+  q.groups = a.groups;
+  q.group_begin = a.group_begin;
+  q.device = a.device;
+  q.P = a.P;
+  if ((err = quantize_t<float>(q, stream)) != hipSuccess) return err;
+  Int8GemmArgs d = g;
+  d.A = reinterpret_cast<const uint16_t *>(act_q);
+  d.lda = a.F / 2;
+  d.B = reinterpret_cast<const uint16_t *>(a.w_down);
+  d.b_expert_stride = int64_t(a.D) * a.F / 2;
+  d.b_blk_stride = int64_t(a.F) * 16;
+  d.C = static_cast<uint16_t *>(a.out_perm);
+  d.ldc = a.D;
+  d.N = a.D;
+  d.Kdim = a.F / 2;
+  d.a_scale = act_scale;
+  d.row_pair = nullptr;
+  d.b_scale = a.down_scale;
+  d.scale_stride = a.D;
+  if (streams) return launch_int8_stream<true, false>(d, rows, mt_most * (a.D / 64), stream);
+  if (a.D % 256 != 0 && a.D % 192 == 0)  // 192-wide tiles divide D exactly
+    hipLaunchKernelGGL((int8_tiles_kernel<192, kWavesM192, kWavesN192, kEpiInt8, true>), dim3(grid),
+                       dim3(64 * kWavesM192 * kWavesN192), 0, stream, d);
+  else
+    hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8, true>), dim3(grid),
+                       dim3(64 * kWavesM * kWavesN), 0, stream, d);
+  return hipGetLastError();
+}
+
+}  // namespace llep

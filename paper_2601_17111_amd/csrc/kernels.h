@@ -156,6 +156,37 @@ struct NormBwdArgs {
 size_t norm_bwd_workspace_bytes(int64_t T, int32_t D);
 hipError_t launch_block_norm_backward(const NormBwdArgs &a, hipStream_t stream);
 
+// 8-bit rows and products (int8.hip).
+hipError_t launch_quantize_rows(int64_t R, int32_t D, llep_dtype dtype, const void *x, int8_t *q,
+                                int32_t q_bytes, float *scale, hipStream_t stream);
+// w1: null, or the up weights whose rows alternate with those of w0 by 32
+hipError_t launch_pack_int8(int32_t E, int32_t N, int32_t K, const int8_t *w0, const int8_t *w1,
+                            int8_t *out, hipStream_t stream);
+struct Int8MatmulArgs {
+  int64_t M;
+  int32_t N, K, x_bytes;
+  llep_dtype dtype;  // of out
+  const int8_t *x, *w;
+  const float *x_scale, *w_scale;
+  void *out, *ws;
+};
+size_t int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K);
+hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream);
+struct FfnInt8Args {
+  int64_t R;
+  int32_t P, E, D, F, K, device;
+  const int32_t *groups, *group_begin, *row_pair;
+  const int8_t *x_perm, *w_gate_up, *w_down;
+  const float *x_scale, *gate_scale, *up_scale, *down_scale;
+  void *out_perm, *ws;
+};
+size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F);
+hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream);
+// The list of tiles of BM rows of a range's groups (grouped_ffn.hip).
+hipError_t launch_tile_table(const int32_t *groups, const int32_t *group_begin, int32_t cap,
+                             int32_t device, int32_t P, int32_t BM, int4 *tiles, int32_t *n_tiles,
+                             hipStream_t stream);
+
 // Gradient norm and clipping (clip.hip).
 struct ClipArgs {
   int32_t n;

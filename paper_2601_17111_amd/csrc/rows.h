@@ -107,8 +107,8 @@ struct RowReduce {
 };
 
 // ---------------------------------------------------------------------------
-// 8-bit rows: q = rint(v * (127 / max|v|)), scale = max|v| / 127, one division
-// each per row; q * scale stands for v. A row whose largest magnitude is below
+// 8-bit rows: q = rint(v * (127 * (1 / max|v|))), scale = max|v| * (1 / 127),
+// each step rounded to 32 bits; q * scale stands for v. A row whose largest magnitude is below
 // 2^-120 (the reciprocal would leave the range) counts as zero: scale and q
 // are 0. A row with an infinity or a NaN gets the scale NaN and q = 0, so that
 // everything computed from it is NaN.
@@ -121,7 +121,7 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(float most) {
   if (__float_as_uint(most) >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.0f};
   if (most < 0x1p-120f) return {0.0f, 0.0f};
-  return {most / 127.0f, 127.0f / most};
+  return {most * (1.0f / 127.0f), 127.0f * (1.0f / most)};
 }
 
 __device__ __forceinline__ int32_t quantize(float v, RowScale s) {

@@ -22,6 +22,43 @@ def m_local_bytes(groups: Sequence[Sequence[int]], P: int, D: int, F: int,
     return out
 
 
+class Int8Experts:
+    """Expert weights in 8 bits for LLEPLayer.forward_int8, packed once.
+
+    w_gate, w_up [E, F, D] and w_down [E, D, F] int8, rows = output channels,
+    with a float32 scale for each: [E, F], [E, F], [E, D] (llep_quantize_rows
+    on the transposed weights gives both).
+    """
+
+    def __init__(self, w_gate, gate_scale, w_up, up_scale, w_down, down_scale, stream=None):
+        E, F, D = w_gate.shape
+        if tuple(w_up.shape) != (E, F, D) or tuple(w_down.shape) != (E, D, F):
+            raise ValueError("w_gate and w_up are [E, F, D], w_down is [E, D, F]")
+        if (tuple(gate_scale.shape) != (E, F) or tuple(up_scale.shape) != (E, F)
+                or tuple(down_scale.shape) != (E, D)):
+            raise ValueError("scales are [E, F], [E, F] and [E, D]")
+        self.E, self.D, self.F = E, D, F
+        self.gate_up = B.llep_pack_matrix_int8(w_gate, w_up, stream)
+        self.down = B.llep_pack_matrix_int8(w_down, stream=stream)
+        self.gate_scale, self.up_scale, self.down_scale = gate_scale, up_scale, down_scale
+
+    @classmethod
+    def from_weights(cls, w_gate, w_up, w_down, stream=None):
+        """From the weights that llep_pack_weights takes: w_gate, w_up [E, D, F] and w_down
+        [E, F, D] in bf16 or float32."""
+        import torch
+        parts = []
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            for w in (w_gate, w_up, w_down):
+                E, K, N = w.shape
+                rows = w.transpose(1, 2).reshape(E * N, K)
+                q = torch.empty((E * N, K), dtype=torch.int8, device=w.device)
+                scale = torch.empty(E * N, dtype=torch.float32, device=w.device)
+                B.llep_quantize_rows(rows, q, scale)
+                parts += [q.view(E, N, K), scale.view(E, N)]
+            return cls(*parts)
+
+
 class LLEPLayer:
     """Buffers and calls for one layer shape.
 
@@ -88,6 +125,40 @@ class LLEPLayer:
         self.ffn(w_gate_up, w_down, -1 if device is None else device, stream, save_gate_up)
         self.combine(gates, stream)
         return self.y
+
+    def forward_int8(self, ids, gates, x, experts: Int8Experts, device: int = -1, stream=None):
+        """forward() for serving with 8-bit experts (bf16 layers): the tokens to 8 bits, then
+        plan -> permute (of the 8-bit rows) -> grouped FFN in 8 bits -> combine. Returns y.
+        backward() is not available after it."""
+        if not hasattr(self, "x_q"):
+            import torch
+            if self.dtype != torch.bfloat16:
+                raise TypeError("forward_int8 needs a bf16 layer")
+            i8 = dict(dtype=torch.int8, device=self.device)
+            self.x_q = torch.empty((self.T, self.D), **i8)
+            self.x_scale = torch.empty(self.T, dtype=torch.float32, device=self.device)
+            self.x_perm_q = torch.empty((max(self.T * self.K, 1), self.D), **i8)
+            nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
+            self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
+            raise ValueError("the experts do not fit this layer")
+        self.gate_up_device = None
+        B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
+        self.plan(ids, stream)
+        self._permute_int8(ids, gates, stream)
+        B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, self.x_scale,
+                                self.row_pair, experts.gate_up, experts.gate_scale,
+                                experts.up_scale, experts.down, experts.down_scale, self.out_perm,
+                                self.int8_workspace, stream)
+        self.combine(gates, stream)
+        return self.y
+
+    def _permute_int8(self, ids, gates, stream):
+        """The permutation of rows of D bytes, as D / 2 bfloat16."""
+        import torch
+        B.llep_permute(self.params, self.bufs, ids, gates, self.x_q.view(torch.bfloat16),
+                       self.x_perm_q.view(torch.bfloat16), self.gate_perm, self.row_pair,
+                       self.pair_row, stream)
 
     def _saved_covers(self, device: int) -> bool:
         saved = getattr(self, "gate_up_device", None)

@@ -79,3 +79,27 @@ def test_clip():
     assert oracle.clip_gradients(g, 5.0)[1][0][0] == 3.0
     norm, out = oracle.clip_gradients([np.array([np.inf, 1.0])], 1.0)
     assert norm == np.inf and out[0][1] == 1.0
+
+
+def test_int8_rows_and_products():
+    q, s = oracle.quantize_rows([[1.0, -2.0, 0.5, 0.0], [0.0] * 4, [np.inf, 1.0, 2.0, 3.0],
+                                 [1e-37, 0.0, 0.0, 0.0], [0.0, np.nan, 1.0, 1.0]])
+    assert q.tolist() == [[64, -127, 32, 0], [0] * 4, [0] * 4, [0] * 4, [0] * 4]  # 63.5 to even
+    assert s[0] == np.float32(2.0) * (np.float32(1) / np.float32(127)) and s[1] == 0 and s[3] == 0
+    assert np.isnan(s[2]) and np.isnan(s[4])
+    assert oracle.int8_product([[1, -2]], [0.5], [[3, 4], [127, 127]], [1.0, 2.0]).tolist() == \
+        [[-2.5, -127.0]]
+
+
+def test_int8_expert_near_the_real_one():
+    """The 8-bit expert on the values that its bytes stand for, against the SwiGLU expert: apart
+    only by the activation's own rounding, at most half a step for each of the F values."""
+    g = np.random.default_rng(3)
+    n, D, F = 5, 16, 24
+    q = [g.integers(-127, 128, s).astype(np.int8) for s in ((n, D), (F, D), (F, D), (D, F))]
+    sx, sg, su, sd = (g.uniform(0.5, 1.5, k) / 127 for k in (n, F, F, D))
+    got, most = oracle.swiglu_ffn_int8(q[0], sx, q[1], sg, q[2], su, q[3], sd)
+    real = [a.astype(np.float64) * s[:, None] for a, s in zip(q, (sx, sg, su, sd))]
+    want = oracle.swiglu_ffn(real[0], real[1].T, real[2].T, real[3].T)
+    bound = (most / 254)[:, None] * np.abs(real[3]).sum(axis=1)[None, :]
+    assert (np.abs(got - want) <= bound + 1e-12).all() and np.abs(got - want).max() > 0
