@@ -33,13 +33,13 @@ struct QuantArgs {
   int32_t device, P;
 };
 
-template <typename T, int kThreads, int kVec, int kPer>
-__global__ __launch_bounds__(kThreads < kRowWg ? kRowWg : kThreads) void quantize_rows_kernel(
+template <typename T, int kPer, bool kOne>
+__global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void quantize_rows_kernel(
     QuantArgs a) {
-  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
-  __shared__ float lds[RowReduce<kThreads>::kLds];
-  RowReduce<kThreads> red(lds);
-  const int t = threadIdx.x % kThreads;
+  constexpr int kVec = 8;
+  __shared__ double lds[RowReduce<kOne>::kLds];
+  RowReduce<kOne> red(lds);
+  const uint32_t n = kOne ? kWave : blockDim.x, t = kOne ? threadIdx.x % kWave : threadIdx.x;
   const uint32_t D = a.D;
   int64_t r0 = 0, r1 = a.R;
   if (a.groups) {
@@ -48,47 +48,61 @@ __global__ __launch_bounds__(kThreads < kRowWg ? kRowWg : kThreads) void quantiz
     r0 = lo < hi ? a.groups[4 * lo + 2] : 0;
     r1 = lo < hi ? a.groups[4 * (hi - 1) + 2] + a.groups[4 * (hi - 1) + 3] : 0;
   }
-  const int first = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
-  for (int64_t row = r0 + int64_t(blockIdx.x) * kRows + first; row < r1;
-       row += int64_t(gridDim.x) * kRows) {
-    const T *x = static_cast<const T *>(a.x) + row * D;
-    float v[kPer][kVec];
-    float most = 0.0f;
+  const int64_t step = int64_t(gridDim.x) * (kOne ? kRowWaves : 1);
+  int64_t row = r0 + (kOne ? int64_t(blockIdx.x) * kRowWaves +
+                                 __builtin_amdgcn_readfirstlane(threadIdx.x / kWave)
+                           : blockIdx.x);
+  RawVec<T, kVec> next[kPer];
+  auto request = [&]() {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) v[j][i] = 0.0f;
-      if (c < D) load_vec<T, kVec>(x + c, v[j]);
+      const uint32_t c = (j * n + t) * kVec;
+      next[j].zero();
+      if (c < D) next[j].load(static_cast<const T *>(a.x) + row * D + c);
     }
+  };
+  constexpr bool kAhead = kPer == 1;  // else there are no registers for it
+  if (kAhead && row < r1) request();
+  while (row < r1) {
+    if (!kAhead) request();
+    float v[kPer][kVec];
+    uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
 #pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(fabsf(v[j][i]))));
+      for (int i = 0; i < kVec; ++i) {
+        v[j][i] = next[j][i];
+        most = max(most, __float_as_uint(fabsf(v[j][i])));
+      }
+    const int64_t at = row;
+    row += step;
+    if (kAhead && row < r1) request();  // the next row, while this one is worked on
     const RowScale s = row_scale(red.max_bits(most));
-    store_int8_row<kThreads, kVec, kPer>(a.q + row * a.q_bytes, D, a.q_bytes, t, v, s);
-    if (t == 0) a.scale[row] = s.scale;
+    store_int8_row<kVec, kPer>(a.q + at * a.q_bytes, D, a.q_bytes, t, n, v, s);
+    if (t == 0) a.scale[at] = s.scale;
   }
 }
 
-// Odd rows too long for the registers: read once for the maximum, again from
-// the cache for the values.
+// Odd rows: not whole 16-byte vectors, or not on 16-byte boundaries. Read
+// element by element, once for the maximum and again from the cache.
 template <typename T>
-__global__ __launch_bounds__(1024) void quantize_long_rows_kernel(QuantArgs a) {
-  __shared__ float lds[RowReduce<1024>::kLds];
-  RowReduce<1024> red(lds);
+__global__ __launch_bounds__(1024) void quantize_odd_rows_kernel(QuantArgs a) {
+  __shared__ double lds[RowReduce<false>::kLds];
+  RowReduce<false> red(lds);
+  const int n = blockDim.x;
   for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
     const T *x = static_cast<const T *>(a.x) + row * a.D;
-    float most = 0.0f;
-    for (int c = threadIdx.x; c < a.D; c += 1024) {
+    uint32_t most = 0;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < a.D; c += n) {
       float v[1];
       load_vec<T, 1>(x + c, v);
-      most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(fabsf(v[0]))));
+      most = max(most, __float_as_uint(fabsf(v[0])));
     }
     const RowScale s = row_scale(red.max_bits(most));
     int8_t *q = a.q + row * a.q_bytes;
-    for (int c = threadIdx.x; c < a.q_bytes; c += 1024) {
+#pragma unroll 4
+    for (int c = threadIdx.x; c < a.q_bytes; c += n) {
       float v[1] = {0.0f};
       if (c < a.D) load_vec<T, 1>(x + c, v);
       q[c] = c < a.D ? int8_t(quantize(v[0], s)) : int8_t(0);
@@ -97,30 +111,30 @@ __global__ __launch_bounds__(1024) void quantize_long_rows_kernel(QuantArgs a) {
   }
 }
 
-template <typename T, int kThreads, int kVec, int kPer>
+constexpr int kQuantWaves = 24;  // of a compute unit that the grid is sized for
+
+template <typename T, int kPer, bool kOne>
 hipError_t run_quantize(const QuantArgs &a, hipStream_t stream) {
-  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
-  const int64_t grid = std::min<int64_t>((a.R + kRows - 1) / kRows, 65536);
-  hipLaunchKernelGGL((quantize_rows_kernel<T, kThreads, kVec, kPer>), dim3(uint32_t(grid)),
-                     dim3(kRows * kThreads), 0, stream, a);
+  const int threads = kOne ? kRowWaves * kWave : row_threads(a.D, 8, kPer);
+  const int64_t wgs = kOne ? (a.R + kRowWaves - 1) / kRowWaves : a.R;
+  const int64_t grid = std::min<int64_t>(wgs, 256 * std::max(1, kQuantWaves * kWave / threads));
+  hipLaunchKernelGGL((quantize_rows_kernel<T, kPer, kOne>), dim3(uint32_t(grid)), dim3(threads), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
-  const int32_t D = a.D;
   if (a.R == 0) return hipSuccess;
-  if (D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0) {
-    if (D <= 2048) return run_quantize<T, 256, 8, 1>(a, stream);
-    if (D <= 4096) return run_quantize<T, 256, 8, 2>(a, stream);
-    if (D <= 8192) return run_quantize<T, 256, 8, 4>(a, stream);
-    return run_quantize<T, 1024, 8, 8>(a, stream);
-  }
-  if (D <= 1024) return run_quantize<T, 256, 1, 4>(a, stream);
-  if (D <= 8192) return run_quantize<T, 1024, 1, 8>(a, stream);
   // (a range of groups has rows of whole vectors: F % 64 == 0)
-  hipLaunchKernelGGL(quantize_long_rows_kernel<T>, dim3(uint32_t(std::min<int64_t>(a.R, 65536))),
-                     dim3(1024), 0, stream, a);
+  if (a.D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0) {
+    static_assert(LLEP_MAX_FFN_DIM == 1024 * 8 * 8, "a row fits a workgroup");
+    if (a.D <= 512) return run_quantize<T, 1, true>(a, stream);
+    if (a.D <= 8192) return run_quantize<T, 1, false>(a, stream);
+    return run_quantize<T, 8, false>(a, stream);
+  }
+  hipLaunchKernelGGL(quantize_odd_rows_kernel<T>, dim3(uint32_t(std::min<int64_t>(a.R, 65536))),
+                     dim3(std::min(1024, (a.D + kWave - 1) / kWave * kWave)), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -19,87 +19,119 @@
 
 namespace llep {
 
-constexpr int64_t kNormGrid = 65536;  // workgroups at most; they then take several rows
+constexpr int kVec = 8;  // elements of a thread's vectors
 
-__device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }
-__device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
-
-template <typename T, int kVec>
-__device__ __forceinline__ void gate_vec(const NormArgs &a, int64_t row, uint32_t c,
-                                         float (&g)[kVec]) {
-  const T *p = static_cast<const T *>(a.gate);
-  if (a.gate_shape == LLEP_GATE_CHANNEL) {
-    load_vec<T, kVec>(p + c, g);
-  } else if (a.gate_shape == LLEP_GATE_FULL) {
-    load_vec<T, kVec>(p + row * a.D + c, g);
-  } else {
-    float v[1] = {1.0f};
-    if (a.gate_shape == LLEP_GATE_TOKEN) load_vec<T, 1>(p + row, v);
+// The weights of a thread's columns (norm weights, and the gate where it
+// varies by channel alone), read once per workgroup.
+template <typename T, int kPer>
+struct ColumnWeights {
+  RawVec<T, kVec> post[kPer], pre[kPer], gate[kPer];
+  __device__ __forceinline__ ColumnWeights(const NormArgs &a, uint32_t t, uint32_t n) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) g[i] = v[0];
+    for (int j = 0; j < kPer; ++j) {
+      const uint32_t c = (j * n + t) * kVec;
+      post[j].zero();
+      pre[j].zero();
+      gate[j].zero();
+      if (c >= uint32_t(a.D)) continue;
+      if (a.w_post) post[j].load(static_cast<const T *>(a.w_post) + c);
+      if (a.w_pre) pre[j].load(static_cast<const T *>(a.w_pre) + c);
+      if (a.gate_shape == LLEP_GATE_CHANNEL) gate[j].load(static_cast<const T *>(a.gate) + c);
+    }
   }
-}
+};
 
-template <typename T, int kThreads, int kVec, int kPer>
-__global__ __launch_bounds__(kThreads < kRowWg ? kRowWg : kThreads) void block_norm_kernel(
-    NormArgs a) {
-  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
-  __shared__ float lds[RowReduce<kThreads>::kLds];
-  RowReduce<kThreads> red(lds);
-  const int t = threadIdx.x % kThreads;
+// The gate's values of one row (requested with the row).
+template <typename T, int kPer>
+struct RowGate {
+  RawVec<T, kVec> full[kPer];
+  float token;
+  __device__ __forceinline__ void load(const NormArgs &a, int64_t row, uint32_t t, uint32_t n) {
+    const T *p = static_cast<const T *>(a.gate);
+    token = 1.0f;
+    if (a.gate_shape == LLEP_GATE_TOKEN) {
+      float v[1];
+      llep::load_vec<T, 1>(p + row, v);
+      token = v[0];
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const uint32_t c = (j * n + t) * kVec;
+      full[j].zero();
+      if (a.gate_shape == LLEP_GATE_FULL && c < uint32_t(a.D)) full[j].load(p + row * a.D + c);
+    }
+  }
+  __device__ __forceinline__ float at(const NormArgs &a, const ColumnWeights<T, kPer> &w, int j,
+                                      int i) const {
+    return a.gate_shape == LLEP_GATE_CHANNEL ? w.gate[j][i]
+           : a.gate_shape == LLEP_GATE_FULL  ? full[j][i]
+                                             : token;
+  }
+};
+
+template <typename T, int kPer, bool kOne>
+__global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_kernel(NormArgs a) {
+  __shared__ double lds[RowReduce<kOne>::kLds];
+  RowReduce<kOne> red(lds);
+  using Raw = RawVec<T, kVec>;
+  const uint32_t n = kOne ? kWave : blockDim.x, t = kOne ? threadIdx.x % kWave : threadIdx.x;
   const uint32_t D = a.D;
   const float per_d = 1.0f / float(D);
   const T *w_post = static_cast<const T *>(a.w_post), *w_pre = static_cast<const T *>(a.w_pre);
-  const int first = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
-  for (int64_t row = int64_t(blockIdx.x) * kRows + first; row < a.T;
-       row += int64_t(gridDim.x) * kRows) {
-    const T *x = static_cast<const T *>(a.x) + row * a.D;
-    float r[kPer][kVec];
+  const int64_t step = int64_t(gridDim.x) * (kOne ? kRowWaves : 1);
+  int64_t row = kOne ? int64_t(blockIdx.x) * kRowWaves +
+                           __builtin_amdgcn_readfirstlane(threadIdx.x / kWave)
+                     : blockIdx.x;
+  Raw x[kPer], b[kPer];
+  RowGate<T, kPer> gate;
+  auto request = [&]() {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) r[j][i] = 0.0f;
-      if (c < D) load_vec<T, kVec>(x + c, r[j]);
+      const uint32_t c = (j * n + t) * kVec;
+      x[j].zero();
+      b[j].zero();
+      if (c >= D) continue;
+      x[j].load(static_cast<const T *>(a.x) + row * D + c);
+      if (a.b) b[j].load(static_cast<const T *>(a.b) + row * D + c);
     }
+    gate.load(a, row, t, n);
+  };
+  if (row < a.T) request();
+  const ColumnWeights<T, kPer> w(a, t, n);
+  while (row < a.T) {
+    float r[kPer][kVec];
     if (a.b) {
-      const T *b = static_cast<const T *>(a.b) + row * a.D;
-      float v[kPer][kVec];
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = (j * kThreads + t) * kVec;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[j][i] = 0.0f;
-        if (c < D) load_vec<T, kVec>(b + c, v[j]);
-      }
       float s = a.alpha;
       if (w_post) {
         float q[1] = {0.0f};
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) q[0] = fmaf(v[j][i], v[j][i], q[0]);
+          for (int i = 0; i < kVec; ++i) q[0] = fmaf(b[j][i], b[j][i], q[0]);
         red.sum(q);
         s *= rsqrtf(q[0] * per_d + a.eps);
       }
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = (j * kThreads + t) * kVec;
-        if (c >= D) continue;
-        float g[kVec], w[kVec];
-        gate_vec<T, kVec>(a, row, c, g);
-        if (w_post) load_vec<T, kVec>(w_post + c, w);
+      for (int j = 0; j < kPer; ++j)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          r[j][i] = fmaf(v[j][i] * s, w_post ? g[i] * w[i] : g[i], r[j][i]);
-      }
+        for (int i = 0; i < kVec; ++i) {
+          const float g = gate.at(a, w, j, i);
+          r[j][i] = fmaf(b[j][i] * s, w_post ? g * w.post[j][i] : g, x[j][i]);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) r[j][i] = x[j][i];
     }
+    const int64_t base = row * D;
+    row += step;
+    if (row < a.T) request();  // the next row, while this one is worked on
     if (a.r) {
-      T *o = static_cast<T *>(a.r) + row * a.D;
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = (j * kThreads + t) * kVec;
-        if (c < D) store_vec<T, kVec>(o + c, r[j]);
+        const uint32_t c = (j * n + t) * kVec;
+        if (c < D) store_vec<T, kVec>(static_cast<T *>(a.r) + base + c, r[j]);
       }
     }
     if (w_pre) {
@@ -112,158 +144,295 @@ __global__ __launch_bounds__(kThreads < kRowWg ? kRowWg : kThreads) void block_n
       const float s = rsqrtf(q[0] * per_d + a.eps);
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = (j * kThreads + t) * kVec;
-        if (c >= D) continue;
-        float w[kVec];
-        load_vec<T, kVec>(w_pre + c, w);
+        const uint32_t c = (j * n + t) * kVec;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) r[j][i] *= s * w[i];
-        if (a.h) store_vec<T, kVec>(static_cast<T *>(a.h) + row * a.D + c, r[j]);
+        for (int i = 0; i < kVec; ++i) r[j][i] *= s * w.pre[j][i];
+        if (a.h && c < D) store_vec<T, kVec>(static_cast<T *>(a.h) + base + c, r[j]);
       }
       if (a.h_q) {
-        float most = 0.0f;
+        uint32_t most = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
 #pragma unroll
-          for (int i = 0; i < kVec; ++i)
-            most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(fabsf(r[j][i]))));
-        const RowScale s = row_scale(red.max_bits(most));
-        store_int8_row<kThreads, kVec, kPer>(a.h_q + row * a.q_bytes, a.D, a.q_bytes, t, r, s);
-        if (t == 0) a.h_scale[row] = s.scale;
+          for (int i = 0; i < kVec; ++i) most = max(most, __float_as_uint(fabsf(r[j][i])));
+        const RowScale s8 = row_scale(red.max_bits(most));
+        const int64_t at = (row - step);
+        store_int8_row<kVec, kPer>(a.h_q + at * a.q_bytes, D, a.q_bytes, t, n, r, s8);
+        if (t == 0) a.h_scale[at] = s8.scale;
       }
     }
   }
 }
 
-// Backward. A workgroup (or wavefront) takes rows g, g + G, ... and keeps the
-// column sums of the weight gradients in registers; they go to the workspace
-// as one row of [2][D] per workgroup, which norm_columns_kernel adds up in a
-// fixed order. The two sums: sum_t d h r i_r, and s = sum_t [g] D b i_b, with
-// the gate inside only where it varies along t. With a gate per channel (or
-// none) d w_post = alpha g s and d g = alpha w_post s: one sum serves both.
-template <typename T, int kThreads, int kVec, int kPer>
-__global__ __launch_bounds__(kThreads) void block_norm_bwd_kernel(NormBwdArgs a) {
-  // In short rows a norm's gradient is the small rest of large terms (with one
-  // element, f eps / (b^2 + eps)), so the path that takes odd rows, which is
-  // not the fast one, has its row sums and what they enter in 64 bits.
-  using A = std::conditional_t<kVec == 1, double, float>;
-  __shared__ A lds[RowReduce<kThreads, A>::kLds];
-  RowReduce<kThreads, A> red(lds);
-  const int t = threadIdx.x;
-  const A per_d = A(1) / A(a.n.D);
+// Backward. A workgroup takes rows g, g + G, ... (the next one is requested
+// while the present one is worked on) and keeps the column sums of the weight
+// gradients in registers; they go to the workspace as one row of [2][D] per
+// workgroup, which norm_columns_kernel adds up in a fixed order. The two sums:
+// sum_t d h r i_r, and s = sum_t [g] D b i_b, with the gate inside only where
+// it varies along t. With a gate per channel (or none) d w_post = alpha g s
+// and d g = alpha w_post s: one sum serves both.
+template <typename T, int kPer, int kMaxThreads>
+__global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs a) {
+  using Raw = RawVec<T, kVec>;
+  __shared__ double lds[RowReduce<false>::kLds];
+  RowReduce<false> red(lds);
+  const uint32_t n = blockDim.x, t = threadIdx.x;
   const uint32_t D = a.n.D;
+  const float per_d = 1.0f / float(D);
   const bool varies = a.n.gate_shape == LLEP_GATE_TOKEN || a.n.gate_shape == LLEP_GATE_FULL;
-  const T *w_post = static_cast<const T *>(a.n.w_post), *w_pre = static_cast<const T *>(a.n.w_pre);
+  const bool has_post = a.n.w_post != nullptr, has_pre = a.n.w_pre != nullptr;
   float sum_pre[kPer][kVec], sum_post[kPer][kVec];
 #pragma unroll
   for (int j = 0; j < kPer; ++j)
 #pragma unroll
     for (int i = 0; i < kVec; ++i) sum_pre[j][i] = sum_post[j][i] = 0.0f;
-  for (int64_t row = blockIdx.x; row < a.n.T; row += gridDim.x) {
+  Raw next_r[kPer], next_b[kPer], next_dr[kPer], next_dh[kPer];
+  RowGate<T, kPer> next_gate;
+  auto request = [&](int64_t row) {
     const int64_t base = row * D;
-    float r[kPer][kVec], b[kPer][kVec], dr[kPer][kVec], dh[kPer][kVec];
-    // sums over the row: r^2, e r, b^2
-    A q[3] = {A(0), A(0), A(0)};
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) r[j][i] = b[j][i] = dr[j][i] = dh[j][i] = 0.0f;
+      const uint32_t c = (j * n + t) * kVec;
+      next_r[j].zero();
+      next_b[j].zero();
+      next_dr[j].zero();
+      next_dh[j].zero();
       if (c >= D) continue;
-      load_vec<T, kVec>(static_cast<const T *>(a.d_r) + base + c, dr[j]);
-      if (w_pre) {
-        load_vec<T, kVec>(static_cast<const T *>(a.r) + base + c, r[j]);
-        load_vec<T, kVec>(static_cast<const T *>(a.d_h) + base + c, dh[j]);
+      next_dr[j].load(static_cast<const T *>(a.d_r) + base + c);
+      if (has_pre) {
+        next_r[j].load(static_cast<const T *>(a.r) + base + c);
+        next_dh[j].load(static_cast<const T *>(a.d_h) + base + c);
       }
-      if (a.n.b) load_vec<T, kVec>(static_cast<const T *>(a.n.b) + base + c, b[j]);
+      if (a.n.b) next_b[j].load(static_cast<const T *>(a.n.b) + base + c);
     }
+    next_gate.load(a.n, row, t, n);
+  };
+  constexpr bool kAhead = kPer == 1;  // else there are no registers for it
+  if (kAhead && blockIdx.x < a.n.T) request(blockIdx.x);
+  const ColumnWeights<T, kPer> w(a.n, t, n);
+  for (int64_t row = blockIdx.x; row < a.n.T; row += gridDim.x) {
+    if (!kAhead) request(row);
+    const int64_t base = row * D;
+    Raw r[kPer], b[kPer], dh[kPer];
+    float dr[kPer][kVec];
+    const RowGate<T, kPer> gate = next_gate;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-      if (c >= D) continue;
-      float w[kVec];
-      if (w_pre) load_vec<T, kVec>(w_pre + c, w);
+      r[j] = next_r[j];
+      b[j] = next_b[j];
+      dh[j] = next_dh[j];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) dr[j][i] = next_dr[j][i];
+    }
+    if (kAhead && row + gridDim.x < a.n.T) request(row + gridDim.x);
+    // sums over the row: r^2, e r, b^2
+    float q[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        if (w_pre) {
-          q[0] += A(r[j][i]) * A(r[j][i]);
-          q[1] += A(dh[j][i]) * A(w[i]) * A(r[j][i]);
-        }
-        q[2] += A(b[j][i]) * A(b[j][i]);
+        q[0] = fmaf(r[j][i], r[j][i], q[0]);
+        q[1] = fmaf(dh[j][i] * w.pre[j][i], r[j][i], q[1]);
+        q[2] = fmaf(b[j][i], b[j][i], q[2]);
       }
-    }
-    if (w_pre || w_post) red.sum(q);
-    const A i_b = w_post ? inv_sqrt(q[2] * per_d + A(a.n.eps)) : A(1);
-    if (w_pre) {
-      const A i_r = inv_sqrt(q[0] * per_d + A(a.n.eps));
-      const A k = i_r * i_r * i_r * (q[1] * per_d);
+    if (has_pre || has_post) red.sum(q);
+    const float i_b = has_post ? rsqrtf(q[2] * per_d + a.n.eps) : 1.0f;
+    if (has_pre) {
+      const float i_r = rsqrtf(q[0] * per_d + a.n.eps);
+      const float k = i_r * i_r * i_r * (q[1] * per_d);
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = (j * kThreads + t) * kVec;
-        if (c >= D) continue;
-        float w[kVec];
-        load_vec<T, kVec>(w_pre + c, w);
+      for (int j = 0; j < kPer; ++j)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-          sum_pre[j][i] = fmaf(dh[j][i], r[j][i] * float(i_r), sum_pre[j][i]);
-          dr[j][i] = float(A(dr[j][i]) + (i_r * (A(dh[j][i]) * A(w[i])) - k * A(r[j][i])));
+          sum_pre[j][i] = fmaf(dh[j][i], r[j][i] * i_r, sum_pre[j][i]);
+          dr[j][i] += fmaf(i_r, dh[j][i] * w.pre[j][i], -k * r[j][i]);
         }
-      }
     }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
+      const uint32_t c = (j * n + t) * kVec;
       if (c < D) store_vec<T, kVec>(static_cast<T *>(a.dx) + base + c, dr[j]);
     }
     if (!a.n.b) continue;
     // f . b / alpha, and D . n (d g of a gate per token)
-    A p[2] = {A(0), A(0)};
+    float p[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-      if (c >= D) continue;
-      float g[kVec], w[kVec];
-      gate_vec<T, kVec>(a.n, row, c, g);
-      if (w_post) load_vec<T, kVec>(w_post + c, w);
+      const uint32_t c = (j * n + t) * kVec;
       float dg[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        const float bi = b[j][i] * float(i_b);
-        const float wi = w_post ? w[i] : 1.0f;
-        sum_post[j][i] = fmaf(varies ? dr[j][i] * g[i] : dr[j][i], bi, sum_post[j][i]);
+        const float bi = b[j][i] * i_b;
+        const float wi = has_post ? w.post[j][i] : 1.0f;
+        const float g = gate.at(a.n, w, j, i);
+        sum_post[j][i] = fmaf(varies ? dr[j][i] * g : dr[j][i], bi, sum_post[j][i]);
         dg[i] = a.n.alpha * dr[j][i] * (bi * wi);
-        p[1] += A(dg[i]);
-        dr[j][i] *= g[i] * wi;  // f / alpha from here on
-        p[0] += A(dr[j][i]) * A(b[j][i]);
+        p[1] += dg[i];
+        dr[j][i] *= g * wi;  // f / alpha from here on
+        p[0] = fmaf(dr[j][i], b[j][i], p[0]);
       }
-      if (a.n.gate_shape == LLEP_GATE_FULL) store_vec<float, kVec>(a.d_gate + base + c, dg);
+      if (a.n.gate_shape == LLEP_GATE_FULL && c < D)
+        store_vec<float, kVec>(a.d_gate + base + c, dg);
     }
-    A k = A(0);
-    if (w_post || a.n.gate_shape == LLEP_GATE_TOKEN) {
+    float k = 0.0f;
+    if (has_post || a.n.gate_shape == LLEP_GATE_TOKEN) {
       red.sum(p);
-      if (w_post) k = i_b * i_b * (p[0] * per_d);
-      if (a.n.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = float(p[1]);
+      if (has_post) k = i_b * i_b * (p[0] * per_d);
+      if (a.n.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = p[1];
     }
-    const A s = A(a.n.alpha) * i_b;
+    const float s = a.n.alpha * i_b;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const uint32_t c = (j * kThreads + t) * kVec;
-      if (c >= D) continue;
+      const uint32_t c = (j * n + t) * kVec;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dr[j][i] = float(s * (A(dr[j][i]) - k * A(b[j][i])));
-      store_vec<T, kVec>(static_cast<T *>(a.db) + base + c, dr[j]);
+      for (int i = 0; i < kVec; ++i) dr[j][i] = s * fmaf(-k, b[j][i], dr[j][i]);
+      if (c < D) store_vec<T, kVec>(static_cast<T *>(a.db) + base + c, dr[j]);
     }
   }
   float *part = a.parts + int64_t(blockIdx.x) * 2 * D;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const uint32_t c = (j * kThreads + t) * kVec;
+    const uint32_t c = (j * n + t) * kVec;
     if (c >= D) continue;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       if (a.dw_pre) part[c + i] = sum_pre[j][i];
       if (a.column_sums) part[D + c + i] = sum_post[j][i];
     }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Odd rows: not whole 16-byte vectors, or not on 16-byte boundaries. Element by
+// element, several times over the row, which the cache holds; what has to stay
+// in 32 bits between two sweeps is kept in LDS, every element by its thread. In
+// short rows a norm's gradient is the small rest of large terms (with one
+// element, f eps / (b^2 + eps)), so the backward, which need not be fast here,
+// has its row sums and what they enter in 64 bits.
+// ---------------------------------------------------------------------------
+
+template <typename T>
+__device__ __forceinline__ float load1(const void *p, int64_t i) {
+  float v[1];
+  load_vec<T, 1>(static_cast<const T *>(p) + i, v);
+  return v[0];
+}
+template <typename T>
+__device__ __forceinline__ void store1(void *p, int64_t i, float v) {
+  const float x[1] = {v};
+  store_vec<T, 1>(static_cast<T *>(p) + i, x);
+}
+template <typename T>
+__device__ __forceinline__ float gate1(const NormArgs &a, int64_t row, int c) {
+  switch (a.gate_shape) {
+    case LLEP_GATE_CHANNEL: return load1<T>(a.gate, c);
+    case LLEP_GATE_TOKEN: return load1<T>(a.gate, row);
+    case LLEP_GATE_FULL: return load1<T>(a.gate, row * a.D + c);
+    default: return 1.0f;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void block_norm_odd_kernel(NormArgs a) {
+  __shared__ double lds[RowReduce<false>::kLds];
+  __shared__ float kept[LLEP_MAX_NORM_DIM];
+  RowReduce<false> red(lds);
+  const int n = blockDim.x, t = threadIdx.x, D = a.D;
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const int64_t base = row * D;
+    float s = a.alpha;
+    if (a.w_post) {
+      float q[1] = {0.0f};
+      for (int c = t; c < D; c += n) {
+        const float b = load1<T>(a.b, base + c);
+        q[0] = fmaf(b, b, q[0]);
+      }
+      red.sum(q);
+      s *= rsqrtf(q[0] / float(D) + a.eps);
+    }
+    float q[1] = {0.0f};
+    for (int c = t; c < D; c += n) {
+      float r = load1<T>(a.x, base + c);
+      if (a.b) {
+        const float g = gate1<T>(a, row, c);
+        r = fmaf(load1<T>(a.b, base + c) * s, a.w_post ? g * load1<T>(a.w_post, c) : g, r);
+      }
+      q[0] = fmaf(r, r, q[0]);
+      kept[c] = r;
+      if (a.r) store1<T>(a.r, base + c, r);
+    }
+    if (!a.w_pre) continue;
+    red.sum(q);
+    s = rsqrtf(q[0] / float(D) + a.eps);
+    uint32_t most = 0;
+    for (int c = t; c < D; c += n) {
+      const float h = kept[c] * (s * load1<T>(a.w_pre, c));
+      most = max(most, __float_as_uint(fabsf(h)));
+      kept[c] = h;
+      if (a.h) store1<T>(a.h, base + c, h);
+    }
+    if (!a.h_q) continue;
+    const RowScale s8 = row_scale(red.max_bits(most));
+    for (int c = t; c < a.q_bytes; c += n)
+      a.h_q[row * a.q_bytes + c] = c < D ? int8_t(quantize(kept[c], s8)) : int8_t(0);
+    if (t == 0) a.h_scale[row] = s8.scale;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void block_norm_bwd_odd_kernel(NormBwdArgs a) {
+  __shared__ double lds[RowReduce<false>::kLds];
+  __shared__ float kept[LLEP_MAX_NORM_DIM];
+  RowReduce<false> red(lds);
+  const NormArgs &f = a.n;
+  const int n = blockDim.x, t = threadIdx.x, D = f.D;
+  const bool varies = f.gate_shape == LLEP_GATE_TOKEN || f.gate_shape == LLEP_GATE_FULL;
+  float *part = a.parts + int64_t(blockIdx.x) * 2 * D;
+  for (int64_t row = blockIdx.x; row < f.T; row += gridDim.x) {
+    const int64_t base = row * D;
+    const bool fresh = row == blockIdx.x;
+    double q[3] = {0.0, 0.0, 0.0};
+    for (int c = t; c < D; c += n) {
+      if (f.w_pre) {
+        const double r = load1<T>(a.r, base + c);
+        q[0] += r * r;
+        q[1] += double(load1<T>(a.d_h, base + c)) * double(load1<T>(f.w_pre, c)) * r;
+      }
+      const double b = f.b ? load1<T>(f.b, base + c) : 0.0;
+      q[2] += b * b;
+    }
+    red.sum(q);
+    const double i_b = f.w_post ? 1.0 / sqrt(q[2] / D + double(f.eps)) : 1.0;
+    const double i_r = 1.0 / sqrt(q[0] / D + double(f.eps));
+    double k = i_r * i_r * i_r * (q[1] / D);
+    double p[2] = {0.0, 0.0};  // f . b / alpha, and D . n
+    for (int c = t; c < D; c += n) {
+      float dr = load1<T>(a.d_r, base + c);
+      if (f.w_pre) {
+        const float r = load1<T>(a.r, base + c), dh = load1<T>(a.d_h, base + c);
+        part[c] = (fresh ? 0.0f : part[c]) + dh * (r * float(i_r));
+        dr = float(double(dr) + (i_r * (double(dh) * double(load1<T>(f.w_pre, c))) - k * double(r)));
+      }
+      store1<T>(a.dx, base + c, dr);
+      if (!f.b) continue;
+      const float b = load1<T>(f.b, base + c), bi = b * float(i_b);
+      const float g = gate1<T>(f, row, c), w = f.w_post ? load1<T>(f.w_post, c) : 1.0f;
+      if (a.column_sums)
+        part[D + c] = (fresh ? 0.0f : part[D + c]) + (varies ? dr * g : dr) * bi;
+      const float dg = f.alpha * dr * (bi * w);
+      if (f.gate_shape == LLEP_GATE_FULL) a.d_gate[base + c] = dg;
+      dr *= g * w;
+      kept[c] = dr;
+      p[0] += double(dr) * double(b);
+      p[1] += double(dg);
+    }
+    if (!f.b) continue;
+    red.sum(p);
+    if (f.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = float(p[1]);
+    k = f.w_post ? i_b * i_b * (p[0] / D) : 0.0;
+    for (int c = t; c < D; c += n)
+      store1<T>(a.db, base + c, float(double(f.alpha) * i_b *
+                                      (double(kept[c]) - k * double(load1<T>(f.b, base + c)))));
   }
 }
 
@@ -277,16 +446,19 @@ __global__ __launch_bounds__(kColumnWaves * kWave) void norm_columns_kernel(Norm
   __shared__ float lds[kColumnWaves][kWave];
   const int D = a.n.D;
   const int which = blockIdx.y;  // 0: d w_pre, 1: the sum of d w_post and d g
+  if (which == 0 ? a.dw_pre == nullptr : !a.column_sums) return;
   const int c = blockIdx.x * kWave + threadIdx.x % kWave, w = threadIdx.x / kWave;
   float s = 0.0f;
-  if (c < D)
+  if (c < D) {
+#pragma unroll 8
     for (int p = w; p < n_parts; p += kColumnWaves) s += a.parts[(int64_t(p) * 2 + which) * D + c];
+  }
   lds[w][threadIdx.x % kWave] = s;
   __syncthreads();
   if (w != 0 || c >= D) return;
   for (int i = 1; i < kColumnWaves; ++i) s += lds[i][threadIdx.x];
   if (which == 0) {
-    if (a.dw_pre) a.dw_pre[c] = s;
+    a.dw_pre[c] = s;
     return;
   }
   float g[1] = {1.0f}, wp[1] = {1.0f};
@@ -298,17 +470,8 @@ __global__ __launch_bounds__(kColumnWaves * kWave) void norm_columns_kernel(Norm
 }
 
 // ---------------------------------------------------------------------------
-// launch: kThreads x kVec x kPer covers a row (at most LLEP_MAX_NORM_DIM = 8192 elements)
+// launch
 // ---------------------------------------------------------------------------
-
-template <typename T, int kThreads, int kVec, int kPer>
-hipError_t run_norm(const NormArgs &a, hipStream_t stream) {
-  constexpr int kRows = kThreads < kRowWg ? kRowWg / kThreads : 1;
-  const int64_t grid = std::min((a.T + kRows - 1) / kRows, kNormGrid);
-  hipLaunchKernelGGL((block_norm_kernel<T, kThreads, kVec, kPer>), dim3(uint32_t(grid)),
-                     dim3(kRows * kThreads), 0, stream, a);
-  return hipGetLastError();
-}
 
 bool rows_aligned(int32_t D, std::initializer_list<const void *> ps) {
   uintptr_t u = 0;
@@ -316,17 +479,33 @@ bool rows_aligned(int32_t D, std::initializer_list<const void *> ps) {
   return D % 8 == 0 && (u & 15) == 0;
 }
 
+// Wavefronts of a compute unit that the grids are sized for. Workgroups stay
+// and take several rows, the next row requested ahead. (8 / 16 / 24 / 32: forward of
+// 16384 x 2880 bf16 106 / 79 / 84 / 79 us, backward 131 / 119 / 146 / 147.)
+constexpr int kNormWaves = 16;
+
+// threads for a row of D elements, one by one
+static int odd_threads(int32_t D) { return std::min(1024, (D + kWave - 1) / kWave * kWave); }
+
+template <typename T, int kPer, bool kOne>
+hipError_t run_norm(const NormArgs &a, hipStream_t stream) {
+  const int threads = kOne ? kRowWaves * kWave : row_threads(a.D, kVec, kPer);
+  const int64_t wgs = kOne ? (a.T + kRowWaves - 1) / kRowWaves : a.T;
+  const int64_t grid = std::min<int64_t>(wgs, int64_t(256) * std::max(1, kNormWaves * kWave / threads));
+  hipLaunchKernelGGL((block_norm_kernel<T, kPer, kOne>), dim3(uint32_t(grid)), dim3(threads), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t stream) {
-  const int32_t D = a.D;
-  if (rows_aligned(D, {a.x, a.b, a.gate_shape == LLEP_GATE_TOKEN ? nullptr : a.gate, a.w_post,
-                       a.w_pre, a.r, a.h})) {
-    if (D <= 2048) return run_norm<T, 256, 8, 1>(a, stream);
-    if (D <= 4096) return run_norm<T, 256, 8, 2>(a, stream);
-    return run_norm<T, 256, 8, 4>(a, stream);
-  }
-  if (D <= 1024) return run_norm<T, 256, 1, 4>(a, stream);
-  return run_norm<T, 1024, 1, 8>(a, stream);
+  static_assert(LLEP_MAX_NORM_DIM == 1024 * kVec, "a row fits a workgroup");
+  if (rows_aligned(a.D, {a.x, a.b, a.gate_shape == LLEP_GATE_TOKEN ? nullptr : a.gate, a.w_post,
+                         a.w_pre, a.r, a.h}))
+    return a.D <= kWave * kVec ? run_norm<T, 1, true>(a, stream) : run_norm<T, 1, false>(a, stream);
+  hipLaunchKernelGGL(block_norm_odd_kernel<T>, dim3(uint32_t(std::min<int64_t>(a.T, 65536))),
+                     dim3(odd_threads(a.D)), 0, stream, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream) {
@@ -334,37 +513,50 @@ hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream) {
   return a.dtype == LLEP_BF16 ? launch_norm_t<uint16_t>(a, stream) : launch_norm_t<float>(a, stream);
 }
 
-size_t norm_bwd_workspace_bytes(int64_t T, int32_t D) {
-  return size_t(std::min<int64_t>(T, kNormBwdGrid)) * 2 * size_t(D) * 4;
+// Workgroups of the backward: one per row up to 256; beyond, at least four rows
+// each, so that the rows of column sums stay a small part of what is moved.
+static int norm_bwd_grid(int64_t T, int32_t D) {
+  if (T <= 256) return int(T);
+  const int waves = row_threads(D, kVec, 1) / kWave;
+  const int64_t most =
+      int64_t(256) * std::max(1, std::min(kNormWaves / waves, kNormBwdGrid / 256));
+  return int(std::max<int64_t>(256, std::min(most, T / 4)));
 }
 
-template <typename T, int kThreads, int kVec, int kPer>
-hipError_t run_norm_bwd(const NormBwdArgs &a, hipStream_t stream) {
-  const int grid = int(std::min<int64_t>(a.n.T, kNormBwdGrid));
-  if (grid > 0) {
-    hipLaunchKernelGGL((block_norm_bwd_kernel<T, kThreads, kVec, kPer>), dim3(grid), dim3(kThreads),
-                       0, stream, a);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-  }
-  if (a.dw_pre || a.column_sums)  // with no rows: zeros
-    hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((a.n.D + kWave - 1) / kWave, 2),
-                       dim3(kColumnWaves * kWave), 0, stream, a, grid);
-  return hipGetLastError();
+size_t norm_bwd_workspace_bytes(int64_t T, int32_t D) {
+  return size_t(norm_bwd_grid(T, D)) * 2 * size_t(D) * 4;
 }
 
 template <typename T>
 hipError_t launch_norm_bwd_t(const NormBwdArgs &a, hipStream_t stream) {
   const int32_t D = a.n.D;
-  if (rows_aligned(D, {a.r, a.n.b, a.n.gate_shape == LLEP_GATE_TOKEN ? nullptr : a.n.gate,
-                       a.n.w_post, a.n.w_pre, a.d_r, a.d_h, a.dx, a.db,
-                       a.n.gate_shape == LLEP_GATE_FULL ? a.d_gate : nullptr})) {
-    if (D <= 2048) return run_norm_bwd<T, 256, 8, 1>(a, stream);
-    if (D <= 4096) return run_norm_bwd<T, 256, 8, 2>(a, stream);
-    return run_norm_bwd<T, 1024, 8, 1>(a, stream);
+  const int grid = norm_bwd_grid(a.n.T, D);
+  if (grid > 0) {
+    const bool whole =
+        rows_aligned(D, {a.r, a.n.b, a.n.gate_shape == LLEP_GATE_TOKEN ? nullptr : a.n.gate,
+                         a.n.w_post, a.n.w_pre, a.d_r, a.d_h, a.dx, a.db,
+                         a.n.gate_shape == LLEP_GATE_FULL ? a.d_gate : nullptr});
+    // 128 registers a thread, as 16 wavefronts have, hold a bf16 row's vectors
+    // and the next row's; long float32 rows take half the threads
+    if (!whole)
+      hipLaunchKernelGGL(block_norm_bwd_odd_kernel<T>, dim3(grid), dim3(odd_threads(D)), 0, stream,
+                         a);
+    else if (D <= 512 * kVec)
+      hipLaunchKernelGGL((block_norm_bwd_kernel<T, 1, 512>), dim3(grid),
+                         dim3(row_threads(D, kVec, 1)), 0, stream, a);
+    else if constexpr (sizeof(T) == 2)
+      hipLaunchKernelGGL((block_norm_bwd_kernel<T, 1, 1024>), dim3(grid),
+                         dim3(row_threads(D, kVec, 1)), 0, stream, a);
+    else
+      hipLaunchKernelGGL((block_norm_bwd_kernel<T, 2, 512>), dim3(grid),
+                         dim3(row_threads(D, kVec, 2)), 0, stream, a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
   }
-  if (D <= 1024) return run_norm_bwd<T, 256, 1, 4>(a, stream);
-  return run_norm_bwd<T, 512, 1, 16>(a, stream);
+  if (a.dw_pre || a.column_sums)  // with no rows: zeros
+    hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((D + kWave - 1) / kWave, 2),
+                       dim3(kColumnWaves * kWave), 0, stream, a, grid);
+  return hipGetLastError();
 }
 
 hipError_t launch_block_norm_backward(const NormBwdArgs &a, hipStream_t stream) {

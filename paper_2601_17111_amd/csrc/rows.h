@@ -1,15 +1,22 @@
 // Rows held in registers: what the kernels that work row by row share (block
-// norms, 8-bit rows). A row of D elements belongs to kThreads threads (a
-// wavefront, or a whole workgroup); thread t holds the kPer vectors of kVec
-// elements at (j * kThreads + t) * kVec, j < kPer, as floats. Everything a
-// row needs is read once; sums over it are of 32 bits or more.
+// norms, 8-bit rows). A row of D elements belongs to n threads, a workgroup of
+// just as many wavefronts as cover it, or one wavefront of four; thread t
+// holds the kPer vectors of kVec elements at (j n + t) kVec, j < kPer.
+// Everything a row needs is read once; sums over it are of 32 bits or more.
 #pragma once
+
+#include <type_traits>
 
 #include "common.h"
 
 namespace llep {
 
-constexpr int kRowWg = 256;  // threads of a workgroup that works on one row per wavefront
+// Threads for a row: a wavefront per 64 kPer vectors. Rows of one wavefront
+// share workgroups of four (no barriers between them).
+constexpr int kRowWaves = 4;
+inline int row_threads(int32_t D, int vec, int per) {
+  return (D + kWave * vec * per - 1) / (kWave * vec * per) * kWave;
+}
 
 // One vector of kVec elements as floats (8: 16-byte accesses, rows that start
 // on 16-byte boundaries and are whole vectors; 1: any row).
@@ -38,6 +45,36 @@ __device__ __forceinline__ void load_vec(const T *p, float (&v)[kVec]) {
   }
 }
 
+// The same vector as it lies in memory, for rows that are read ahead of their
+// use, and as floats.
+template <typename T, int kVec>
+struct RawVec {
+  static constexpr int kWords = kVec == 1 ? 1 : int(sizeof(T)) * kVec / 16;
+  using Word = std::conditional_t<kVec == 1, T, i32x4>;
+  Word w[kWords];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = Word{};
+  }
+  __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const Word *>(p)[i];
+  }
+  __device__ __forceinline__ float operator[](int i) const {  // i: known when compiled
+    if constexpr (kVec == 1) {
+      if constexpr (sizeof(T) == 2)
+        return bf16_to_f32(w[0]);
+      else
+        return w[0];
+    } else if constexpr (sizeof(T) == 2) {
+      const uint32_t u = uint32_t(w[0][i / 2]);
+      return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+    } else {
+      return __int_as_float(w[i / 4][i % 4]);
+    }
+  }
+};
+
 template <typename T, int kVec>
 __device__ __forceinline__ void store_vec(T *p, const float (&v)[kVec]) {
   if constexpr (kVec == 1) {
@@ -59,50 +96,91 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[kVec]) {
   }
 }
 
-// Sums and maxima over the threads of a row, the same in every thread and on
-// every run. The LDS halves alternate from one reduction to the next: a half
-// is written again only after the barrier of the reduction between.
-template <int kThreads, typename V = float>
-struct RowReduce {
-  static constexpr int kWaves = kThreads / kWave;
-  static constexpr int kMost = 4;  // values per reduction
-  static constexpr int kLds = kWaves > 1 ? 2 * kWaves * kMost : 1;
-  V *lds;
-  int half = 0;
-  __device__ __forceinline__ explicit RowReduce(V *lds_) : lds(lds_) {}
+// v of the lane that the DPP control names, or 0 where there is none
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), kCtrl, kRowMask, 0xf, false));
+}
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(dpp<kCtrl, kRowMask>(__float_as_uint(v)));
+}
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t(dpp<kCtrl, kRowMask>(uint32_t(u >> 32))) << 32) |
+                                        dpp<kCtrl, kRowMask>(uint32_t(u)));
+}
+__device__ __forceinline__ uint32_t read_lane(uint32_t v, int lane) {
+  return uint32_t(__builtin_amdgcn_readlane(int(v), lane));
+}
+__device__ __forceinline__ float read_lane(float v, int lane) {
+  return __uint_as_float(read_lane(__float_as_uint(v), lane));
+}
+__device__ __forceinline__ double read_lane(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t(read_lane(uint32_t(u >> 32), lane)) << 32) |
+                                        read_lane(uint32_t(u), lane));
+}
 
-  template <int N, class Op>
+// Sum (or, of unsigned integers, maximum) over the wavefront's first 16 lanes
+// (kAll false) or all 64, in every lane and always in the same order: shifts
+// within the rows of 16 lanes, then from row to row. 0 is neutral for both.
+template <bool kAll, int N, typename V, class Op>
+__device__ __forceinline__ void wave_reduce(V (&v)[N], Op op) {
+#define LLEP_DPP_STEP(ctrl, rows) \
+  _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = op(v[i], dpp<ctrl, rows>(v[i]));
+  LLEP_DPP_STEP(0x111, 0xf)  // row_shr:1, :2, :4, :8
+  LLEP_DPP_STEP(0x112, 0xf)
+  LLEP_DPP_STEP(0x114, 0xf)
+  LLEP_DPP_STEP(0x118, 0xf)
+  if constexpr (kAll) {
+    LLEP_DPP_STEP(0x142, 0xa)  // row_bcast:15, :31
+    LLEP_DPP_STEP(0x143, 0xc)
+  }
+#undef LLEP_DPP_STEP
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = read_lane(v[i], kAll ? 63 : 15);
+}
+
+// Sums and maxima over the wavefronts of a workgroup (at most 16) or, with
+// kOne, over one wavefront; the same in every thread and on every run. The LDS
+// halves alternate from one reduction to the next: a half is written again
+// only after the barrier of the reduction between.
+template <bool kOne>
+struct RowReduce {
+  static constexpr int kMost = 4;  // values per reduction
+  static constexpr int kLds = kOne ? 1 : 2 * 16 * kMost;  // of 8 bytes
+  double *lds;
+  int half = 0;
+  __device__ __forceinline__ explicit RowReduce(double *lds_) : lds(lds_) {}
+
+  template <int N, typename V, class Op>
   __device__ __forceinline__ void reduce(V (&v)[N], Op op) {
     static_assert(N <= kMost, "room in LDS");
-#pragma unroll
-    for (int o = kWave / 2; o >= 1; o >>= 1)
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = op(v[i], __shfl_xor(v[i], o));
-    if constexpr (kWaves > 1) {
-      V *s = lds + half * kWaves * kMost;
+    wave_reduce<true>(v, op);
+    if constexpr (!kOne) {
+      V *s = reinterpret_cast<V *>(lds + half * 16 * kMost);
       half ^= 1;
-      if (lane_id() == 0)
+      const int lane = lane_id(), waves = blockDim.x / kWave;
+      if (lane == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[threadIdx.x / kWave * kMost + i] = v[i];
+        for (int i = 0; i < N; ++i) s[i * 16 + threadIdx.x / kWave] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = s[i];
-      for (int w = 1; w < kWaves; ++w)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = op(v[i], s[w * kMost + i]);
+      for (int i = 0; i < N; ++i) v[i] = lane < waves ? s[i * 16 + (lane & 15)] : V(0);
+      wave_reduce<false>(v, op);
     }
   }
-  template <int N>
+  template <int N, typename V>
   __device__ __forceinline__ void sum(V (&v)[N]) {
     reduce(v, [](V a, V b) { return a + b; });
   }
   // the largest by the bits of non-negative floats: NaN above infinity
-  __device__ __forceinline__ float max_bits(float v) {
-    float x[1] = {v};
-    reduce(x, [](float a, float b) {
-      return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
-    });
-    return x[0];
+  __device__ __forceinline__ float max_bits(uint32_t bits) {
+    uint32_t x[1] = {bits};
+    reduce(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+    return __uint_as_float(x[0]);
   }
 };
 
@@ -130,14 +208,14 @@ __device__ __forceinline__ int32_t quantize(float v, RowScale s) {
   return s.inv != 0.0f ? int32_t(q) : 0;
 }
 
-// Vector j of thread t of an 8-bit row of `bytes` bytes (a multiple of 64):
-// elements from D on are zero.
-template <int kThreads, int kVec, int kPer>
-__device__ __forceinline__ void store_int8_row(int8_t *row, int32_t D, int32_t bytes, int t,
+// The vectors of thread t of n of an 8-bit row of `bytes` bytes (a multiple of
+// 64): elements from D on are zero.
+template <int kVec, int kPer>
+__device__ __forceinline__ void store_int8_row(int8_t *row, int32_t D, int32_t bytes, int t, int n,
                                                const float (&v)[kPer][kVec], RowScale s) {
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const int c = (j * kThreads + t) * kVec;
+    const int c = (j * n + t) * kVec;
     if constexpr (kVec == 8) {
       if (c < D) {
         uint32_t w[2] = {0u, 0u};
@@ -149,7 +227,7 @@ __device__ __forceinline__ void store_int8_row(int8_t *row, int32_t D, int32_t b
       if (c < D) row[c] = int8_t(quantize(v[j][0], s));
     }
   }
-  for (int c = D + t; c < bytes; c += kThreads) row[c] = 0;
+  for (int c = D + t; c < bytes; c += n) row[c] = 0;
 }
 
 }  // namespace llep
