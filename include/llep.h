@@ -451,8 +451,8 @@ int llep_quantize_rows(int64_t R, int32_t D, llep_dtype dtype, const void *x,
 
 /* Packed 8-bit weights (untimed setup): per expert (E = 1: one matrix) rows
  * w[n][k], n < N output channels, in blocks of 16 rows x 64 k: element (n, k)
- * at ((n/16) * (K'/64) + k/64) * 1024 + (n%16) * 64 + k%64, K' = K rounded up
- * to a multiple of 64, zeros in rows from N and columns from K on.
+ * at ((n/16) * (K'/64) + k/64) * 1024 + (k%64/16) * 256 + (n%16) * 16 + k%16,
+ * K' = K rounded up to a multiple of 64, zeros in rows from N and columns from K on.
  * w [E][N][K]; with w_up [E][N][K] (N % 32 == 0) the matrix has 2N rows: row
  * 64j + c is row 32j + c of w (the gate), row 64j + 32 + c row 32j + c of w_up.
  * packed: llep_packed_int8_bytes(E, N, K) bytes, twice that with w_up; 0 for

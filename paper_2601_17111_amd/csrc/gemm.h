@@ -292,11 +292,11 @@ __device__ __forceinline__ bool decode_tile(const GemmArgs &g, int u, int n_mt, 
   return true;
 }
 
-// Byte size of the LDS ring of a 256 x BN tile (kStages stages of A and B
+// Byte size of the LDS ring of a BM x BN tile (kStages stages of A and B
 // slices).
-template <int BN>
+template <int BN, int BM = 256>
 constexpr uint32_t ring_bytes() {
-  return uint32_t(kStages) * (256 * kSK * 2 + BN * kSK * 2);
+  return uint32_t(kStages) * (BM * kSK * 2 + BN * kSK * 2);
 }
 
 // Tile hand-out of a persistent launch, as the tile loop below sees it:
@@ -310,12 +310,14 @@ constexpr uint32_t ring_bytes() {
 //              more: another tile of this loop follows);
 //   kOpaqueLane  whether the lane index is hidden from the compiler's hoisting;
 //   kCoherentC whether C is stored device-coherent (read by other tiles of
-//              the same launch).
+//              the same launch);
+//   kBM        rows of a tile.
 //
 // LaunchSched serves a launch of one problem: tiles (it * G + slot) of the
 // tile order.
 template <int BM, int BN>
 struct LaunchSched {
+  static constexpr int kBM = BM;
   static constexpr bool kOpaqueLane = false;
   static constexpr bool kCoherentC = false;  // C is read only by later launches
   GemmArgs g;  // a copy (no reference to the kernel argument: its fields
@@ -350,7 +352,7 @@ struct LaunchSched {
 template <int BN, int WAVES_M, int WAVES_N, int kEpi, bool kABlocked, bool kCBlocked,
           class Sched, class Args>
 __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t, Sched &sched) {
-  constexpr int BM = 256;
+  constexpr int BM = Sched::kBM;
   constexpr int NW = WAVES_M * WAVES_N;
   constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N;
   constexpr int TM = WM / 32, TN = WN / 32;
@@ -379,7 +381,7 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
   // stage s: A rows at s * STAGE_BYTES, then B rows; the last two stages are
   // also the epilogue's staging area
   constexpr uint32_t STAGE_BYTES = A_STAGE_BYTES + B_STAGE_BYTES;
-  static_assert(kStages * STAGE_BYTES == ring_bytes<BN>(), "ring size");
+  static_assert(kStages * STAGE_BYTES == ring_bytes<BN, BM>(), "ring size");
   auto stageA = [&](int st) { return reinterpret_cast<const uint16_t *>(smem + st * STAGE_BYTES); };
   auto stageB = [&](int st) {
     return reinterpret_cast<const uint16_t *>(smem + st * STAGE_BYTES + A_STAGE_BYTES);
@@ -406,6 +408,9 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
     asm volatile("" : "+v"(ln));
     const int kc_load = (ln & 3) ^ ((ln >> 4) & 3);
     const int32_t blk_lane = (ln >> 2) * 64 + kc_load * 16;
+    // (packed 8-bit weights lie chunk after chunk, 16 rows each, and stay so in
+    // LDS: a fragment's 16 rows are 256 contiguous bytes)
+    const int32_t b_lane = kInt8 ? ln * 16 : blk_lane;
     // rows (columns) past the tile's valid ones re-read its last valid row
     // (block), so every address stays in bounds
     if (kABlocked) {
@@ -432,7 +437,7 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
 #pragma unroll
     for (int j = 0; j < B_SLOTS; ++j) {
       const int nb = min(wave + NWD * j, (c.cols_valid - 1) >> 4);
-      offB[j] = int32_t(nb * g.b_blk_stride + blk_lane);
+      offB[j] = int32_t(nb * g.b_blk_stride + b_lane);
     }
   };
   // request slice kt into stage st: 64 B per row along K for a row-major A,
@@ -463,6 +468,9 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
   // read from LDS while the current one feeds the MFMAs, so LDS latency hides
   // behind the MFMAs.
   static_assert(kSK == 32, "two k-steps per slice");
+  auto b_index = [&](int row, int kc) {  // in 2-byte elements of a stage
+    return kInt8 ? (row >> 4) * 512 + kc * 128 + (row & 15) * 8 : lds_swz32(row, kc);
+  };
   auto mfma = [](const Frag &b, const Frag &a, const Acc &c) {
     if constexpr (kInt8)
       return __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, c, 0, 0, 0);
@@ -478,7 +486,7 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
       fa[i] = *reinterpret_cast<const Frag *>(&a_s[lds_swz32(wm * WM + i * 32 + (lane & 31), kc)]);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-      fb[j] = *reinterpret_cast<const Frag *>(&b_s[lds_swz32(wn * WN + j * 32 + (lane & 31), kc)]);
+      fb[j] = *reinterpret_cast<const Frag *>(&b_s[b_index(wn * WN + j * 32 + (lane & 31), kc)]);
   };
   auto mfma_step = [&](Acc (&acc)[TM][TN], const Frag (&fa)[TM], const Frag (&fb)[TN]) {
 #pragma unroll
@@ -512,7 +520,7 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
     } else if (q < NR) {
       const uint16_t *b_s = stageB(st_next);
       fb[q - TM] = *reinterpret_cast<const Frag *>(
-          &b_s[lds_swz32(wn * WN + (q - TM) * 32 + (lane & 31), ks_next * 2 + (lane >> 5))]);
+          &b_s[b_index(wn * WN + (q - TM) * 32 + (lane & 31), ks_next * 2 + (lane >> 5))]);
     } else if constexpr (kDmaWave) {
       const int d = dma_lo + q - NR;
       const uint32_t a_st = sA0 + st_dma * STAGE_BYTES, b_st = sB0 + st_dma * STAGE_BYTES;

@@ -189,6 +189,7 @@ static_assert(kClaimWave >= kWavesM * kWavesN / 2 && kClaimWave < kWavesM * kWav
 // 1: down-projection tiles of width BN2) of the single launch.
 template <int kPhase, int BN1, int BN2>
 struct FusedSched {
+  static constexpr int kBM = 256;
   static constexpr int BN = kPhase == 0 ? BN1 : BN2;
   static constexpr bool kOpaqueLane = false;
   static constexpr bool kCoherentC = kPhase == 0;  // the activations

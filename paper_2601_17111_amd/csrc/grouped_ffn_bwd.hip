@@ -239,6 +239,7 @@ struct WgSched {
 };
 
 struct DxSched {
+  static constexpr int kBM = 256;
   static constexpr bool kOpaqueLane = true;  // two loops: registers are short
   static constexpr bool kCoherentC = false;  // C is read only by later launches
   const GemmArgs &g;

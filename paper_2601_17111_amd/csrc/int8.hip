@@ -4,14 +4,16 @@
 // the sum exact in 32-bit integers, so that a result does not depend on which
 // kernel ran or how k was split.
 //
-// Weights are packed (llep_pack_int8) in blocks of 16 rows x 64 k, 1 KB each:
-// a matrix-core operand of 16 rows is one contiguous block. Two kernels:
+// Weights are packed (llep_pack_int8) in blocks of 16 rows x 64 k, 1 KB each,
+// 16 bytes of each row after another: lane l of a wavefront that reads a block
+// in order has what it needs as a matrix-core operand of 16 rows. Two kernels:
 //   - tiles (gemm.h): 256 x 256 or 256 x 192 outputs per workgroup, operands
 //     through a ring in LDS, bound by the matrix cores;
 //   - stream (below): every wavefront reads its operands from memory straight
 //     into registers and the wavefronts of a workgroup split k, for few rows,
 //     where reading the weights once is the work.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm.h"
 #include "rows.h"
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(1024) void quantize_odd_rows_kernel(QuantArgs a) {
     for (int c = threadIdx.x; c < a.q_bytes; c += n) {
       float v[1] = {0.0f};
       if (c < a.D) load_vec<T, 1>(x + c, v);
-      q[c] = c < a.D ? int8_t(quantize(v[0], s)) : int8_t(0);
+      q[c] = c < a.D ? quantize(v[0], s) : int8_t(0);
     }
     if (threadIdx.x == 0) a.scale[row] = s.scale;
   }
@@ -165,8 +167,8 @@ __global__ __launch_bounds__(256) void pack_int8_kernel(const int8_t *__restrict
     const int kbs = Kp / 64;
     const int kb = int(blk % kbs), nb = int(blk / kbs % (Np / 16));
     const int64_t e = blk / kbs / (Np / 16);
-    int n = nb * 16 + (int(i) >> 2 & 15);
-    const int k = kb * 64 + (int(i) & 3) * 16;
+    int n = nb * 16 + (int(i) & 15);
+    const int k = kb * 64 + (int(i) >> 4 & 3) * 16;
     // two matrices: 32 rows of the first, then the matching 32 of the second
     const int8_t *src = w0;
     bool ok = n < N;
@@ -209,16 +211,32 @@ hipError_t launch_pack_int8(int32_t E, int32_t N, int32_t K, const int8_t *w0, c
 // rows of the weights; a workgroup of kWaves wavefronts takes one item at a
 // time, each wavefront a part of k, and adds the parts up through LDS.
 // v_mfma_i32_16x16x64_i8 takes a 1 KB block of the weights as its first
-// operand (lane l: row l % 16, bytes 16 (l / 16) .. + 15 of its 64), 16 rows of
-// A likewise as its second; lane l then holds, of row l % 16 of A, the columns
-// 4 (l / 16) .. + 3.
+// operand (lane l: row l % 16, bytes 16 (l / 16) .. + 15 of its 64: the block in
+// order; rows of 64 bytes one after another took 10% longer), 16 rows of A as
+// its second; lane l then holds, of row l % 16 of A, the columns
+// 4 (l / 16) .. + 3. Every XCD (workgroups are dealt round-robin over the 8)
+// takes a contiguous eighth of the items: dense ones with the row tiles of a
+// weight unit next to each other, so that its weights come to one L2 once;
+// grouped ones with the units of a row tile next to each other.
 // ---------------------------------------------------------------------------
 
-template <int kMB, int kNB, int kWaves, bool kGrouped, bool kSwigluOut>
+template <int kMB, int kNB, int kWaves, bool kGrouped, bool kSwigluOut, bool kOnce>
 __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArgs g) {
-  constexpr int kUnroll = kMB * kNB >= 8 ? 2 : 4;  // blocks of k requested together
-  __shared__ i32x4 part[kWaves][kMB * kNB][kWave];
-  static_assert(!kSwigluOut || kNB == 4, "32 gate rows and the matching 32 up rows");
+  constexpr int kBlocks = kMB * kNB;
+  // With more than 16 rows, A goes through LDS (kStaged): a wavefront that
+  // reads 16 rows for an operand touches 16 lines with every quarter of its
+  // lanes, four times the work of the same bytes in order.
+  constexpr bool kStaged = kMB > 1;
+  // blocks of k requested together, and 16 x 16 blocks of the outputs whose
+  // parts are in LDS at a time
+  constexpr int kUnroll = kStaged ? 1 : 4;
+  constexpr int kRound = kBlocks >= 16 ? 8 : kBlocks;
+  constexpr int kStage = kUnroll * kMB * 1024;  // bytes of A per wavefront, twice
+  constexpr int kLdsBytes = kStaged && 2 * kStage > kRound * 1024 ? 2 * kStage : kRound * 1024;
+  __shared__ __attribute__((aligned(1024))) char lds[kWaves * kLdsBytes];
+  i32x4 (*part)[kRound][kWave] = reinterpret_cast<i32x4 (*)[kRound][kWave]>(lds);
+  static_assert(!kSwigluOut || kNB == 4 || kNB == 2, "gate blocks and the matching up blocks");
+  static_assert(kBlocks % kRound == 0 && kRound % kNB == 0, "rounds of whole rows of blocks");
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int nkb = g.Kdim / 32;               // blocks of 64 k
@@ -226,8 +244,12 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
   const int n_unit = (n_blk + kNB - 1) / kNB;
   const int n_mt = kGrouped ? *g.n_mtiles : int((g.M + 16 * kMB - 1) / (16 * kMB));
   const int kb0 = nkb * wave / kWaves, kb1 = nkb * (wave + 1) / kWaves;
-  for (int64_t item = blockIdx.x; item < int64_t(n_mt) * n_unit; item += gridDim.x) {
-    const int mt = int(item / n_unit), unit = int(item % n_unit);
+  const int64_t items = int64_t(n_mt) * n_unit;
+  const int xcd = blockIdx.x % 8;
+  const int64_t end = items * (xcd + 1) / 8;
+  for (int64_t item = items * xcd / 8 + blockIdx.x / 8; item < end; item += gridDim.x / 8) {
+    const int mt = int(kGrouped ? item / n_unit : item % n_mt);
+    const int unit = int(kGrouped ? item % n_unit : item / n_mt);
     int e = 0;
     int64_t row0 = int64_t(mt) * 16 * kMB;
     int rows;
@@ -241,99 +263,168 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
       rows = int(min<int64_t>(16 * kMB, g.M - row0));
     }
     const int8_t *A = reinterpret_cast<const int8_t *>(g.A) + row0 * g.lda * 2;
-    const int8_t *B = reinterpret_cast<const int8_t *>(g.B) + e * g.b_expert_stride * 2;
+    // first packed block of the unit, and from one of its blocks to the next:
+    // with two blocks a unit is 16 gate rows and the matching up rows
+    constexpr int kApart = kSwigluOut && kNB == 2 ? 2 : 1;
+    const int blk0 = kApart == 2 ? 4 * (unit >> 1) + (unit & 1) : unit * kNB;
+    const int8_t *B = reinterpret_cast<const int8_t *>(g.B) + e * g.b_expert_stride * 2 +
+                      int64_t(blk0) * g.b_blk_stride;
     uint32_t offA[kMB], offB[kNB];
 #pragma unroll
-    for (int m = 0; m < kMB; ++m)
+    for (int m = 0; m < kMB; ++m)  // past the last row: the last one again, not stored
       offA[m] = uint32_t(min(m * 16 + (lane & 15), rows - 1)) * uint32_t(g.lda * 2) + (lane >> 4) * 16;
-    const int8_t *Bu = B + int64_t(unit) * kNB * g.b_blk_stride;
 #pragma unroll
-    for (int n = 0; n < kNB; ++n)  // past the last block: the last one again, not stored
-      offB[n] = uint32_t(min(n, n_blk - 1 - unit * kNB)) * uint32_t(g.b_blk_stride) +
-                (lane & 15) * 64 + (lane >> 4) * 16;
+    for (int n = 0; n < kNB; ++n)  // and past the last block
+      offB[n] = uint32_t(min(n * kApart, n_blk - 1 - blk0)) * uint32_t(g.b_blk_stride) +
+                lane * 16;
+    // kOnce: weights that no later call finds in a cache pass by them
+    auto load_weights = [](const int8_t *p) {
+      if constexpr (kOnce)
+        return __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(p));
+      else
+        return *reinterpret_cast<const i32x4 *>(p);
+    };
     i32x4 acc[kMB][kNB];
 #pragma unroll
     for (int m = 0; m < kMB; ++m)
 #pragma unroll
       for (int n = 0; n < kNB; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
-    auto steps = [&](auto count, int kb) {
-      constexpr int kU = decltype(count)::value;
-      i32x4 fa[kU][kMB], fb[kU][kNB];
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-#pragma unroll
-        for (int n = 0; n < kNB; ++n)
-          fb[u][n] = *reinterpret_cast<const i32x4 *>(Bu + int64_t(kb + u) * 1024 + offB[n]);
-#pragma unroll
-        for (int m = 0; m < kMB; ++m)
-          fa[u][m] = *reinterpret_cast<const i32x4 *>(A + (kb + u) * 64 + offA[m]);
-      }
-#pragma unroll
-      for (int u = 0; u < kU; ++u)
-#pragma unroll
-        for (int m = 0; m < kMB; ++m)
-#pragma unroll
-          for (int n = 0; n < kNB; ++n)
-            acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][n], fa[u][m], acc[m][n], 0, 0, 0);
-    };
-    int kb = kb0;
-    for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
-    for (; kb < kb1; ++kb) steps(std::integral_constant<int, 1>{}, kb);
-    if constexpr (kWaves > 1) {
+    if constexpr (kStaged) {
+      // One step of kUnroll blocks of k ahead: its rows of A on their way to
+      // the wavefront's other half of LDS (lane l: row l / 4 of 16, 16 bytes of
+      // it), its weights to registers; the wait at the top of a step is for
+      // everything, so both are there. No barrier: each wavefront has its own
+      // part of LDS. Blocks past the last one are the last again, not used.
+      const char *stage = lds + wave * kLdsBytes;
+      const uint32_t stage_at = lds_addr(lds) + wave * kLdsBytes;
+      int32_t offS[kMB];
 #pragma unroll
       for (int m = 0; m < kMB; ++m)
+        offS[m] = min(m * 16 + (lane >> 2), rows - 1) * int32_t(g.lda * 2) +
+                  (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
+      i32x4 fb[kUnroll][kNB];
+      auto request = [&](int kb, int half) {
 #pragma unroll
-        for (int n = 0; n < kNB; ++n) part[wave][m * kNB + n][lane] = acc[m][n];
+        for (int u = 0; u < kUnroll; ++u) {
+          const int k = min(kb + u, kb1 - 1);
+#pragma unroll
+          for (int m = 0; m < kMB; ++m)
+            dma16(reinterpret_cast<const char *>(A) + k * 64, offS[m],
+                  stage_at + half * kStage + (u * kMB + m) * 1024);
+#pragma unroll
+          for (int n = 0; n < kNB; ++n)
+            fb[u][n] = *reinterpret_cast<const i32x4 *>(B + int64_t(k) * 1024 + offB[n]);
+        }
+      };
+      if (kb0 < kb1) request(kb0, 0);
+      int half = 0;
+      for (int kb = kb0; kb < kb1; kb += kUnroll) {
+        asm volatile("" ::: "memory");
+        wait_cnt<0, 0>();
+        asm volatile("" ::: "memory");
+        i32x4 now[kUnroll][kNB];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+          for (int n = 0; n < kNB; ++n) now[u][n] = fb[u][n];
+        if (kb + kUnroll < kb1) request(kb + kUnroll, half ^ 1);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (kb + u >= kb1) break;
+#pragma unroll
+          for (int m = 0; m < kMB; ++m) {
+            const int r = lane & 15;
+            const i32x4 fa = *reinterpret_cast<const i32x4 *>(
+                stage + half * kStage + (u * kMB + m) * 1024 + r * 64 +
+                (((lane >> 4) ^ ((r >> 2) & 3)) << 4));
+#pragma unroll
+            for (int n = 0; n < kNB; ++n)
+              acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][n], fa, acc[m][n], 0, 0, 0);
+          }
+        }
+        half ^= 1;
+      }
+      // the parts below go over the stages: every wavefront's reads are done
+      asm volatile("" ::: "memory");
+      wait_cnt<0, 0>();
       __syncthreads();
-    }
-    // the sum over the wavefronts of a 16 x 16 block
-    auto total = [&](int m, int n) {
-      if constexpr (kWaves == 1) {
-        return acc[m][n];
-      } else {
-        i32x4 s = part[0][m * kNB + n][lane];
-        for (int w = 1; w < kWaves; ++w) s += part[w][m * kNB + n][lane];
-        return s;
-      }
-    };
-    if constexpr (kSwigluOut) {
-      const int F = g.N / 2;
-#pragma unroll
-      for (int q = 0; q < kMB * 2; ++q) {  // 16 rows x 16 activation columns
-        if (kWaves > 1 && q % kWaves != wave) continue;
-        const int m = q / 2, half = q % 2;
-        const i32x4 sg = total(m, half), su = total(m, 2 + half);
-        const int r = m * 16 + (lane & 15), col = unit * 32 + half * 16 + (lane >> 4) * 4;
-        if (r >= rows) continue;
-        const float sa = int8_row_scale(g, row0 + r);
-        const f32x4 cg = int8_col_scales(g.b_scale + e * g.scale_stride, col, F);
-        const f32x4 cu = int8_col_scales(g.b_scale2 + e * g.scale_stride, col, F);
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[i] = int8_swiglu(int8_value(sg[i], sa, cg[i]), int8_value(su[i], sa, cu[i]));
-        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(g.C) + (row0 + r) * F + col) = v;
-      }
     } else {
+      auto steps = [&](auto count, int kb) {
+        constexpr int kU = decltype(count)::value;
+        i32x4 fa[kU][kMB], fb[kU][kNB];
 #pragma unroll
-      for (int q = 0; q < kMB * kNB; ++q) {
-        if (kWaves > 1 && q % kWaves != wave) continue;
-        const int m = q / kNB, n = q % kNB;
-        const i32x4 s = total(m, n);
-        const int r = m * 16 + (lane & 15), col = (unit * kNB + n) * 16 + (lane >> 4) * 4;
-        if (r >= rows || col >= g.N) continue;
-        const float sa = int8_row_scale(g, row0 + r);
-        const f32x4 cb = int8_col_scales(g.b_scale + e * g.scale_stride, col, g.N);
-        f32x4 v;
+        for (int u = 0; u < kU; ++u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = int8_value(s[i], sa, cb[i]);
-        if (g.f32_out)
-          int8_store4(reinterpret_cast<float *>(g.C) + (row0 + r) * g.ldc, col, g.N, v);
-        else
-          int8_store4(g.C + (row0 + r) * g.ldc, col, g.N, v);
-      }
+          for (int n = 0; n < kNB; ++n)
+            fb[u][n] = load_weights(B + int64_t(kb + u) * 1024 + offB[n]);
+#pragma unroll
+          for (int m = 0; m < kMB; ++m)
+            fa[u][m] = *reinterpret_cast<const i32x4 *>(A + (kb + u) * 64 + offA[m]);
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int m = 0; m < kMB; ++m)
+#pragma unroll
+            for (int n = 0; n < kNB; ++n)
+              acc[m][n] =
+                  __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][n], fa[u][m], acc[m][n], 0, 0, 0);
+      };
+      int kb = kb0;
+      for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
+      for (; kb < kb1; ++kb) steps(std::integral_constant<int, 1>{}, kb);
     }
-    if constexpr (kWaves > 1) __syncthreads();  // the parts are read before the next item's
+#pragma unroll
+    for (int b0 = 0; b0 < kBlocks; b0 += kRound) {
+#pragma unroll
+      for (int b = 0; b < kRound; ++b)
+        part[wave][b][lane] = acc[(b0 + b) / kNB][(b0 + b) % kNB];
+      __syncthreads();
+      // the sum over the wavefronts of a block
+      auto total = [&](int b) {
+        i32x4 s = part[0][b][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) s += part[w][b][lane];
+        return s;
+      };
+      if constexpr (kSwigluOut) {
+        constexpr int kHalf = kNB / 2;  // blocks of 16 activation columns
+        const int F = g.N / 2;
+        for (int q = wave; q < kRound / 2; q += kWaves) {
+          const int m = q / kHalf, half = q % kHalf;
+          const int r = (b0 / kNB + m) * 16 + (lane & 15);
+          const int col = unit * kHalf * 16 + half * 16 + (lane >> 4) * 4;
+          if (r >= rows) continue;
+          const i32x4 sg = total(m * kNB + half), su = total(m * kNB + kHalf + half);
+          const float sa = int8_row_scale(g, row0 + r);
+          const f32x4 cg = int8_col_scales(g.b_scale + e * g.scale_stride, col, F);
+          const f32x4 cu = int8_col_scales(g.b_scale2 + e * g.scale_stride, col, F);
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] = int8_swiglu(int8_value(sg[i], sa, cg[i]), int8_value(su[i], sa, cu[i]));
+          *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(g.C) + (row0 + r) * F + col) = v;
+        }
+      } else {
+        for (int q = wave; q < kRound; q += kWaves) {
+          const int m = q / kNB, n = q % kNB;
+          const int r = (b0 / kNB + m) * 16 + (lane & 15);
+          const int col = (unit * kNB + n) * 16 + (lane >> 4) * 4;
+          if (r >= rows || col >= g.N) continue;
+          const i32x4 s = total(q);
+          const float sa = int8_row_scale(g, row0 + r);
+          const f32x4 cb = int8_col_scales(g.b_scale + e * g.scale_stride, col, g.N);
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = int8_value(s[i], sa, cb[i]);
+          if (g.f32_out)
+            int8_store4(reinterpret_cast<float *>(g.C) + (row0 + r) * g.ldc, col, g.N, v);
+          else
+            int8_store4(g.C + (row0 + r) * g.ldc, col, g.N, v);
+        }
+      }
+      __syncthreads();  // the parts are read before the next ones
+    }
   }
 }
 
@@ -342,8 +433,9 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
 // ---------------------------------------------------------------------------
 
 // Hand-out of a dense product's tiles: those of LaunchSched, computed from M.
-template <int BN>
+template <int BM, int BN>
 struct DenseSched {
+  static constexpr int kBM = BM;
   static constexpr bool kOpaqueLane = false;
   static constexpr bool kCoherentC = false;
   int64_t M;
@@ -352,7 +444,7 @@ struct DenseSched {
     M = g.M;
     N = g.N;
     nk = g.Kdim / kSK;
-    n_mt = int((M + kTileM - 1) / kTileM);
+    n_mt = int((M + BM - 1) / BM);
     n_nt = (N + BN - 1) / BN;
     G = gridDim.x;
     slot = (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8;
@@ -367,8 +459,8 @@ struct DenseSched {
     t.row0 = 0;
     t.prow0 = 0;
     t.mt = sr * kGroupM + rem % gm;
-    t.m0 = t.mt * kTileM;
-    t.rows_valid = int(min<int64_t>(kTileM, M - t.m0));
+    t.m0 = t.mt * BM;
+    t.rows_valid = int(min<int64_t>(BM, M - t.m0));
     t.n0 = rem / gm * BN;
     t.cols_valid = min(BN, N - t.n0);
     t.nk = nk;
@@ -380,36 +472,60 @@ struct DenseSched {
   __device__ __forceinline__ void done(const TileCoord &, bool) {}
 };
 
-template <int BN, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N)
-__attribute__((amdgpu_waves_per_eu(WAVES_M * WAVES_N / 4, WAVES_M * WAVES_N / 4)))
+// BM x BN tiles: 256 rows by eight wavefronts, one workgroup on a compute unit,
+// or 128 x 128 by four, two workgroups; two wavefronts per SIMD either way.
+template <int BM, int BN, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void int8_tiles_kernel(Int8GemmArgs g) {
-  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes<BN>()];
-  std::conditional_t<kGrouped, LaunchSched<256, BN>, DenseSched<BN>> sched(g);
+  __shared__ __attribute__((aligned(1024))) char smem[ring_bytes<BN, BM>()];
+  std::conditional_t<kGrouped, LaunchSched<BM, BN>, DenseSched<BM, BN>> sched(g);
   TileCoord t;
   if (!sched.first(t)) return;
   gemm_tiles<BN, WAVES_M, WAVES_N, kEpi, false, false>(g, smem, t, sched);
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
+hipError_t run_int8_tiles(const Int8GemmArgs &g, hipStream_t stream) {
+  const int grid = (cu_count() * (BM == 256 ? 1 : 2) + 7) / 8 * 8;
+  hipLaunchKernelGGL((int8_tiles_kernel<BM, BN, WAVES_M, WAVES_N, kEpi, kGrouped>), dim3(grid),
+                     dim3(64 * WAVES_M * WAVES_N), 0, stream, g);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
 // launch
 // ---------------------------------------------------------------------------
 
-// Rows up to which a product takes the stream: 64 per item read the weights
-// once; beyond, tiles do more work per byte.
-constexpr int64_t kInt8StreamRows = 64;
-
-template <bool kGrouped, bool kSwigluOut>
-hipError_t launch_int8_stream(const Int8GemmArgs &g, int64_t rows, int64_t items_most,
-                              hipStream_t stream) {
-  const int grid = int(std::min<int64_t>(items_most, 16384));
-  if (rows <= 16)
-    hipLaunchKernelGGL((int8_stream_kernel<1, 4, 4, kGrouped, kSwigluOut>), dim3(grid), dim3(256), 0,
-                       stream, g);
-  else
-    hipLaunchKernelGGL((int8_stream_kernel<4, 4, 4, kGrouped, kSwigluOut>), dim3(grid), dim3(256), 0,
-                       stream, g);
+template <int kMB, int kNB, int kWaves, bool kGrouped, bool kSwigluOut, bool kOnce>
+hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t stream) {
+  const int64_t items = mtiles * ((g.N + 16 * kNB - 1) / (16 * kNB));
+  const int grid = int(std::min<int64_t>((items + 7) / 8 * 8, 16384));
+  hipLaunchKernelGGL((int8_stream_kernel<kMB, kNB, kWaves, kGrouped, kSwigluOut, kOnce>),
+                     dim3(grid), dim3(kWaves * kWave), 0, stream, g);
   return hipGetLastError();
+}
+
+// The stream for `mtiles` row tiles (at most) of at most `rows` rows: 16, 32 or
+// 64. Up to 16 rows, with few weights, k is split over more wavefronts, so that
+// about 1024 are at work (1 row, N x K = 7168 x 2048 with 4 / 8 / 16
+// wavefronts: 5.6 / 3.8 / 4.7 us; 768 x 7168: 9.4 / - / 4.9 us).
+// bytes: of all weights that the call reads. Beyond half of the 256 MB cache
+// behind the L2s they are read past the caches (16 rows; 15 experts of 2880 x
+// 2880 in use, 376 MB: 105 -> 98 us; 4 experts, 100 MB, the same four in every
+// call: 44 -> 49 us).
+template <bool kGrouped, bool kSwigluOut>
+hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, int64_t bytes,
+                              hipStream_t stream) {
+  constexpr bool G = kGrouped, S = kSwigluOut;
+  if (rows > 32) return run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
+  if (rows > 16) return run_int8_stream<2, 4, 4, G, S, false>(g, mtiles, stream);
+  const int64_t units = mtiles * ((g.N + 63) / 64);  // of 64 packed rows
+  if (units * 4 >= 1024)
+    return bytes > (int64_t(128) << 20) ? run_int8_stream<1, 4, 4, G, S, true>(g, mtiles, stream)
+                                        : run_int8_stream<1, 4, 4, G, S, false>(g, mtiles, stream);
+  if (S || units * 16 >= 1024) return run_int8_stream<1, 2, 8, G, S, false>(g, mtiles, stream);
+  if constexpr (!S) return run_int8_stream<1, 1, 16, G, S, false>(g, mtiles, stream);
+  return hipErrorInvalidValue;
 }
 
 size_t int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K) {
@@ -432,12 +548,19 @@ hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream) {
   g.b_scale = a.w_scale;
   g.M = a.M;
   g.f32_out = a.dtype == LLEP_F32;
-  if (a.M <= kInt8StreamRows)
-    return launch_int8_stream<false, false>(g, a.M, (int64_t(a.N) + 63) / 64, stream);
-  const int grid = (cu_count() + 7) / 8 * 8;
-  hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8, false>), dim3(grid),
-                     dim3(64 * kWavesM * kWavesN), 0, stream, g);
-  return hipGetLastError();
+  // The ring's 256 x 256 tiles take about 1 us per 64 bytes of k however few
+  // there are, one on each compute unit, the stream 2.9 fs per multiply-add:
+  // 2048^3 40 / 26 us, 512 x 7168 x 2048 35 / 21, 512 x 2048 x 7168 66 / 19,
+  // 4096^3 70 / 105 (tiles / stream).
+  const double tiles = double((a.M + 255) / 256) * double((a.N + 255) / 256);
+  const double ring = std::ceil(tiles / cu_count()) * (Kp / 64) * 1.0;
+  const double streamed = 2.9e-9 * double(a.M) * double(a.N) * double(a.K);
+  if (a.M <= 64 || streamed < ring) {
+    const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
+    return launch_int8_stream<false, false>(g, rows, (a.M + rows - 1) / rows,
+                                            int64_t(a.N) * Kp, stream);
+  }
+  return run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8, false>(g, stream);
 }
 
 // Workspace of the grouped FFN: the tile count (int at 0), the tile list, the
@@ -461,6 +584,29 @@ size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F) {
   return int8_ws(R, E, P, F).total;
 }
 
+// Rows of a tile, by the rows per expert on average (the routing is not known
+// here): the stream's 16, 32 or 64, or 128 or 256 rows through the ring. Whole
+// layers in us with 16 / 32 / 64 / 128 / 256 rows, uniform routing:
+//   2880 x 2880, 32 experts, 4 of them a token:
+//     32 tokens 176 / 177 / 182 / 189 / 184, 128 tokens 218 / 193 / 194 / 200 / 201,
+//     300 tokens 352 / 267 / 230 / 226 / 217, 700 tokens 685 / 403 / 344 / 269 / 254
+//   2048 x 768, 128 experts, 8: 128 tokens 149 / 149 / 159 / 167 / 178,
+//     700 tokens 236 / 209 / 197 / 195 / 196, 1500 tokens 378 / 290 / 279 / 220 / 239,
+//     3000 tokens 808 / 458 / 421 / 340 / 302
+//   1024 x 768, 16 experts, 2: 300 tokens 53 / 48 / 48 / 60 / 67,
+//     1500 tokens 75 / 64 / 63 / 64 / 80, 3000 tokens 116 / 95 / 92 / 85 / 88
+// (60% of the pairs on four experts: the same order, closer together.)
+static int ffn_int8_rows(const FfnInt8Args &a) {
+  const int64_t R = a.R, E = a.E;
+  if (R <= 8 * E) return 16;
+  if (R <= 24 * E) return 32;
+  const int64_t weight = int64_t(a.D) * a.F;
+  if (weight * R <= int64_t(3000000000)) return 64;
+  // 128 rows where 256 would be half empty, or too few tiles for the chip
+  const int64_t tiles = (R / 256 + E) * ((a.F + 127) / 128);
+  return (R <= 128 * E && weight <= 2000000) || tiles < 256 ? 128 : 256;
+}
+
 hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   if (a.R == 0) return hipSuccess;
   const Int8Ws w = int8_ws(a.R, a.E, a.P, a.F);
@@ -470,13 +616,12 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   float *act = reinterpret_cast<float *>(ws + w.act);
   int8_t *act_q = reinterpret_cast<int8_t *>(ws + w.act_q);
   float *act_scale = reinterpret_cast<float *>(ws + w.scale);
-  // rows per expert on average (the routing is not known here)
-  const bool streams = a.R <= 24 * int64_t(a.E) && a.R <= 4096;
-  const int rows = !streams ? kTileM : a.R <= 4 * int64_t(a.E) ? 16 : 64;
+  const int rows = ffn_int8_rows(a);
+  const bool streams = rows <= 64;
+  const int64_t bytes = 3 * std::min<int64_t>(a.R, a.E) * a.D * a.F;  // of the weights, at most
   hipError_t err = launch_tile_table(a.groups, a.group_begin, 2 * a.E + a.P, a.device, a.P, rows,
                                      tiles, n_mtiles, stream);
   if (err != hipSuccess) return err;
-  const int grid = (cu_count() + 7) / 8 * 8;
   const int64_t mt_most = a.R / rows + std::min<int64_t>(a.R, 2 * int64_t(a.E) + a.P);
   Int8GemmArgs g = {};
   g.A = reinterpret_cast<const uint16_t *>(a.x_perm);
@@ -498,11 +643,10 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   g.b_scale2 = a.up_scale;
   g.scale_stride = a.F;
   if (streams) {
-    err = launch_int8_stream<true, true>(g, rows, mt_most * (a.F / 32), stream);
+    err = launch_int8_stream<true, true>(g, rows, mt_most, bytes, stream);
   } else {
-    hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8Swiglu, true>), dim3(grid),
-                       dim3(64 * kWavesM * kWavesN), 0, stream, g);
-    err = hipGetLastError();
+    err = rows == 128 ? run_int8_tiles<128, 128, 2, 2, kEpiInt8Swiglu, true>(g, stream)
+                      : run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8Swiglu, true>(g, stream);
   }
   if (err != hipSuccess) return err;
   QuantArgs q = {};
@@ -530,14 +674,9 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   d.row_pair = nullptr;
   d.b_scale = a.down_scale;
   d.scale_stride = a.D;
-  if (streams) return launch_int8_stream<true, false>(d, rows, mt_most * (a.D / 64), stream);
-  if (a.D % 256 != 0 && a.D % 192 == 0)  // 192-wide tiles divide D exactly
-    hipLaunchKernelGGL((int8_tiles_kernel<192, kWavesM192, kWavesN192, kEpiInt8, true>), dim3(grid),
-                       dim3(64 * kWavesM192 * kWavesN192), 0, stream, d);
-  else
-    hipLaunchKernelGGL((int8_tiles_kernel<256, kWavesM, kWavesN, kEpiInt8, true>), dim3(grid),
-                       dim3(64 * kWavesM * kWavesN), 0, stream, d);
-  return hipGetLastError();
+  if (streams) return launch_int8_stream<true, false>(d, rows, mt_most, bytes, stream);
+  if (rows == 128) return run_int8_tiles<128, 128, 2, 2, kEpiInt8, true>(d, stream);
+  return run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8, true>(d, stream);
 }
 
 }  // namespace llep

@@ -374,7 +374,7 @@ __global__ __launch_bounds__(1024) void block_norm_odd_kernel(NormArgs a) {
     if (!a.h_q) continue;
     const RowScale s8 = row_scale(red.max_bits(most));
     for (int c = t; c < a.q_bytes; c += n)
-      a.h_q[row * a.q_bytes + c] = c < D ? int8_t(quantize(kept[c], s8)) : int8_t(0);
+      a.h_q[row * a.q_bytes + c] = c < D ? quantize(kept[c], s8) : int8_t(0);
     if (t == 0) a.h_scale[row] = s8.scale;
   }
 }

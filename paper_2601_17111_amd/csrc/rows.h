@@ -202,10 +202,25 @@ __device__ __forceinline__ RowScale row_scale(float most) {
   return {most * (1.0f / 127.0f), 127.0f * (1.0f / most)};
 }
 
-__device__ __forceinline__ int32_t quantize(float v, RowScale s) {
-  // inv == 0 (zero rows, rows that are not finite): 0 whatever v is
-  const float q = fminf(fmaxf(rintf(v * s.inv), -127.0f), 127.0f);
-  return s.inv != 0.0f ? int32_t(q) : 0;
+__device__ __forceinline__ int8_t quantize(float v, RowScale s) {
+  return int8_t(s.inv != 0.0f ? rintf(v * s.inv) : 0.0f);  // at most 127: inv is rounded once
+}
+
+// Four at a time. v inv + 1.5 * 2^23 has rint(v inv) in its low byte (the sum
+// is rounded to a whole number, ties to even; the product before it, as above,
+// so the two are not contracted).
+__device__ __forceinline__ uint32_t quantize4(const float *v, float inv) {
+#pragma clang fp contract(off)
+  uint32_t q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float p = v[i] * inv;
+    q[i] = __float_as_uint(p + 12582912.0f);
+  }
+  // bytes 0 of each: v_perm_b32 picks from (second operand: 0-3, first: 4-7)
+  const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
+  return lo | hi;
 }
 
 // The vectors of thread t of n of an 8-bit row of `bytes` bytes (a multiple of
@@ -213,19 +228,14 @@ __device__ __forceinline__ int32_t quantize(float v, RowScale s) {
 template <int kVec, int kPer>
 __device__ __forceinline__ void store_int8_row(int8_t *row, int32_t D, int32_t bytes, int t, int n,
                                                const float (&v)[kPer][kVec], RowScale s) {
+  static_assert(kVec == 8, "whole vectors");
+  const bool zero = s.inv == 0.0f;  // whatever the values are
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int c = (j * n + t) * kVec;
-    if constexpr (kVec == 8) {
-      if (c < D) {
-        uint32_t w[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t(quantize(v[j][i], s)) & 255u) << (8 * (i % 4));
-        *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
-      }
-    } else {
-      if (c < D) row[c] = int8_t(quantize(v[j][0], s));
-    }
+    if (c < D)
+      *reinterpret_cast<uint2 *>(row + c) =
+          make_uint2(zero ? 0u : quantize4(v[j], s.inv), zero ? 0u : quantize4(v[j] + 4, s.inv));
   }
   for (int c = D + t; c < bytes; c += n) row[c] = 0;
 }
