@@ -311,13 +311,16 @@ constexpr uint32_t ring_bytes() {
 //   kOpaqueLane  whether the lane index is hidden from the compiler's hoisting;
 //   kCoherentC whether C is stored device-coherent (read by other tiles of
 //              the same launch);
-//   kBM        rows of a tile.
+//   kBM        rows of a tile;
+//   kAnyC      (8-bit) whether C may be float32 or have rows that are not whole
+//              16-byte vectors.
 //
 // LaunchSched serves a launch of one problem: tiles (it * G + slot) of the
 // tile order.
 template <int BM, int BN>
 struct LaunchSched {
   static constexpr int kBM = BM;
+  static constexpr bool kAnyC = false;
   static constexpr bool kOpaqueLane = false;
   static constexpr bool kCoherentC = false;  // C is read only by later launches
   GemmArgs g;  // a copy (no reference to the kernel argument: its fields
@@ -377,7 +380,8 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
   static_assert(A_BLOCKS % NWD == 0 && PER_STAGE > 0 && NWD <= NW, "DMA split");
   static_assert(WM % 32 == 0 && WN % 32 == 0, "wave tile");
   static_assert(kAhead == 4, "waits below are written for four slices ahead");
-  static_assert((!kSwiglu && kEpi != kEpiInt8Swiglu) || (WN % 64) == 0, "SwiGLU needs gate/up column pairs per wave");
+  static_assert((!kSwiglu && !kInt8) || (WN % 64) == 0, "SwiGLU needs gate/up column pairs per wave");
+  static_assert(!kInt8 || WM % 64 == 0, "a lane holds the scales of rows 64 apart");
   // stage s: A rows at s * STAGE_BYTES, then B rows; the last two stages are
   // also the epilogue's staging area
   constexpr uint32_t STAGE_BYTES = A_STAGE_BYTES + B_STAGE_BYTES;
@@ -565,6 +569,26 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+    // 8-bit: the scales of the wave's rows (lane l: rows l and l + 64) and
+    // columns (lane l: column l; SwiGLU: of 32 gate columns, then of the up
+    // columns), requested here so that the epilogue need not wait for them
+    constexpr int kRowSets = WM / 64 > 0 ? WM / 64 : 1, kColSets = WN / 64 > 0 ? WN / 64 : 1;
+    [[maybe_unused]] float s_row[kRowSets], s_col[kColSets];
+    if constexpr (kInt8) {
+#pragma unroll
+      for (int i = 0; i < kRowSets; ++i)
+        s_row[i] = int8_row_scale(g, int64_t(t.row0) + t.m0 +
+                                         min(wm * WM + i * 64 + lane, t.rows_valid - 1));
+#pragma unroll
+      for (int j = 0; j < kColSets; ++j) {
+        const int c = t.n0 + wn * WN + j * 64;  // SwiGLU: half as many columns of each
+        if constexpr (kEpi == kEpiInt8Swiglu)
+          s_col[j] = (lane < 32 ? g.b_scale : g.b_scale2)[t.e * g.scale_stride +
+                                                          min(c / 2 + (lane & 31), g.N / 2 - 1)];
+        else
+          s_col[j] = g.b_scale[t.e * g.scale_stride + min(c + lane, g.N - 1)];
+      }
+    }
     // A wave whose 32 x 32 blocks all lie past the tile's last valid row or
     // column (a group's last, partly filled m-tile; the last n-tile) has no
     // MFMA work: it runs the same slice loop with the same DMA requests and
@@ -653,6 +677,14 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
         else
           wait_and_sync<0>();
       }
+    }
+    if constexpr (kInt8) {
+      // the scales have long come; said here, or the compiler would wait for
+      // them in the epilogue and so for the next tile's slices
+#pragma unroll
+      for (float &v : s_row) asm volatile("" : "+v"(v));
+#pragma unroll
+      for (float &v : s_col) asm volatile("" : "+v"(v));
     }
     // every wave is done with the ring before the next tile's slices land
     __syncthreads();
@@ -885,28 +917,33 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
       // float32 activations, row-major by row of A: 32 rows x 32 columns at a
       // time through the staging area, out as whole 128-byte row pieces
       constexpr int RS = 128 + 16;
-      static_assert(32 * RS <= STAGING, "staging");
+      static_assert(32 * RS + 256 <= STAGING, "staging");
       const int F = g.N / 2;
       float *act = reinterpret_cast<float *>(g.C);
+      float *cols = reinterpret_cast<float *>(stg + 32 * RS);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        if (i * 32 >= rows_w) break;
-        const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
-        const float sa = int8_row_scale(g, row0 + min(lane & 31, rows_w - i * 32 - 1));
+      for (int p = 0; p < TN / 2; ++p) {
+        const int f = (c.n0 + wn * WN + p * 64) >> 1;
+        if (f >= F) continue;
+        cols[lane] = s_col[p];
+        f32x4 sg[4], su[4];
 #pragma unroll
-        for (int p = 0; p < TN / 2; ++p) {
-          const int f = (c.n0 + wn * WN + p * 64) >> 1;
-          if (f >= F) continue;
+        for (int gq = 0; gq < 4; ++gq) {
+          sg[gq] = *reinterpret_cast<const f32x4 *>(cols + 8 * gq + 4 * h);
+          su[gq] = *reinterpret_cast<const f32x4 *>(cols + 32 + 8 * gq + 4 * h);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if (i * 32 >= rows_w) break;
+          const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
+          const float sa = __shfl(s_row[i / 2], (i & 1) * 32 + (lane & 31));
 #pragma unroll
           for (int gq = 0; gq < 4; ++gq) {
-            const int col = f + 8 * gq + 4 * h;
-            const f32x4 sg = int8_col_scales(g.b_scale + c.e * g.scale_stride, col, F);
-            const f32x4 su = int8_col_scales(g.b_scale2 + c.e * g.scale_stride, col, F);
             f32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              v[e] = int8_swiglu(int8_value(acc[i][2 * p][4 * gq + e], sa, sg[e]),
-                                 int8_value(acc[i][2 * p + 1][4 * gq + e], sa, su[e]));
+              v[e] = int8_swiglu(int8_value(acc[i][2 * p][4 * gq + e], sa, sg[gq][e]),
+                                 int8_value(acc[i][2 * p + 1][4 * gq + e], sa, su[gq][e]));
             *reinterpret_cast<f32x4 *>(stg + (lane & 31) * RS + (8 * gq + 4 * h) * 4) = v;
           }
 #pragma unroll
@@ -924,22 +961,25 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
       // below; other C (float32, any N) are stored from the registers
       constexpr int RS = WN * 2 + 16;
       constexpr int CH = WN / 8;
-      static_assert(32 * RS <= STAGING, "staging");
+      static_assert(32 * RS + WN * 4 <= STAGING, "staging");
       const int ncol0 = c.n0 + wn * WN;
-      const bool staged = !g.f32_out && (g.N & 7) == 0;
+      const bool staged = !Sched::kAnyC || (!g.f32_out && (g.N & 7) == 0);
+      float *cols = reinterpret_cast<float *>(stg + 32 * RS);
+#pragma unroll
+      for (int j = 0; j < WN / 64; ++j) cols[j * 64 + lane] = s_col[j];
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         if (i * 32 >= rows_w) break;
         const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
         const bool row_ok = i * 32 + (lane & 31) < rows_w;
         const int64_t row = row0 + min(lane & 31, rows_w - i * 32 - 1);
-        const float sa = int8_row_scale(g, row);
+        const float sa = __shfl(s_row[i / 2], (i & 1) * 32 + (lane & 31));
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
           for (int gq = 0; gq < 4; ++gq) {
             const int col = ncol0 + j * 32 + 8 * gq + 4 * h;
-            const f32x4 sb = int8_col_scales(g.b_scale + c.e * g.scale_stride, col, g.N);
+            const f32x4 sb = *reinterpret_cast<const f32x4 *>(cols + j * 32 + 8 * gq + 4 * h);
             f32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = int8_value(acc[i][j][4 * gq + e], sa, sb[e]);

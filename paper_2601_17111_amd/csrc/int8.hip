@@ -436,6 +436,7 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
 template <int BM, int BN>
 struct DenseSched {
   static constexpr int kBM = BM;
+  static constexpr bool kAnyC = true;
   static constexpr bool kOpaqueLane = false;
   static constexpr bool kCoherentC = false;
   int64_t M;
