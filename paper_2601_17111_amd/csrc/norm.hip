@@ -487,11 +487,18 @@ constexpr int kNormWaves = 16;
 // threads for a row of D elements, one by one
 static int odd_threads(int32_t D) { return std::min(1024, (D + kWave - 1) / kWave * kWave); }
 
+// at most `most` workgroups for n rows, with as many rows each
+static int64_t even_grid(int64_t n, int64_t most) {
+  if (n <= most) return n;
+  const int64_t rows = (n + most - 1) / most;
+  return (n + rows - 1) / rows;
+}
+
 template <typename T, int kPer, bool kOne>
 hipError_t run_norm(const NormArgs &a, hipStream_t stream) {
   const int threads = kOne ? kRowWaves * kWave : row_threads(a.D, kVec, kPer);
   const int64_t wgs = kOne ? (a.T + kRowWaves - 1) / kRowWaves : a.T;
-  const int64_t grid = std::min<int64_t>(wgs, int64_t(256) * std::max(1, kNormWaves * kWave / threads));
+  const int64_t grid = even_grid(wgs, int64_t(256) * std::max(1, kNormWaves * kWave / threads));
   hipLaunchKernelGGL((block_norm_kernel<T, kPer, kOne>), dim3(uint32_t(grid)), dim3(threads), 0,
                      stream, a);
   return hipGetLastError();
@@ -513,14 +520,14 @@ hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream) {
   return a.dtype == LLEP_BF16 ? launch_norm_t<uint16_t>(a, stream) : launch_norm_t<float>(a, stream);
 }
 
-// Workgroups of the backward: one per row up to 256; beyond, at least four rows
-// each, so that the rows of column sums stay a small part of what is moved.
+// Workgroups of the backward, all with as many rows (but the last): one row up
+// to 256 workgroups, then four, so that the rows of column sums stay a small
+// part of what is moved, then what the chip has room for.
 static int norm_bwd_grid(int64_t T, int32_t D) {
-  if (T <= 256) return int(T);
   const int waves = row_threads(D, kVec, 1) / kWave;
   const int64_t most =
       int64_t(256) * std::max(1, std::min(kNormWaves / waves, kNormBwdGrid / 256));
-  return int(std::max<int64_t>(256, std::min(most, T / 4)));
+  return int(even_grid(T, std::max<int64_t>(256, std::min(most, (T + 3) / 4))));
 }
 
 size_t norm_bwd_workspace_bytes(int64_t T, int32_t D) {

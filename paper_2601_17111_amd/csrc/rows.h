@@ -49,6 +49,7 @@ __device__ __forceinline__ void load_vec(const T *p, float (&v)[kVec]) {
 // use, and as floats.
 template <typename T, int kVec>
 struct RawVec {
+  static constexpr int kElems = kVec;
   static constexpr int kWords = kVec == 1 ? 1 : int(sizeof(T)) * kVec / 16;
   using Word = std::conditional_t<kVec == 1, T, i32x4>;
   Word w[kWords];
