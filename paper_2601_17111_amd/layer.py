@@ -126,15 +126,18 @@ class LLEPLayer:
         self.combine(gates, stream)
         return self.y
 
-    def forward_int8(self, ids, gates, x, experts: Int8Experts, device: int = -1, stream=None):
+    def forward_int8(self, ids, gates, x, experts: Int8Experts, device: int = -1, stream=None,
+                     x_scale=None):
         """forward() for serving with 8-bit experts (bf16 layers): the tokens to 8 bits, then
         plan -> permute (of the 8-bit rows) -> grouped FFN in 8 bits -> combine. Returns y.
-        backward() is not available after it."""
+        x [T, D] may already be 8-bit rows (int8), with their x_scale [T] (llep_block_norm and
+        llep_quantize_rows write both). backward() is not available after it."""
         if not hasattr(self, "x_q"):
             import torch
             if self.dtype != torch.bfloat16:
                 raise TypeError("forward_int8 needs a bf16 layer")
             i8 = dict(dtype=torch.int8, device=self.device)
+            B.llep_int8_row_bytes(self.D)  # refuses what the 8-bit calls would
             self.x_q = torch.empty((self.T, self.D), **i8)
             self.x_scale = torch.empty(self.T, dtype=torch.float32, device=self.device)
             self.x_perm_q = torch.empty((max(self.T * self.K, 1), self.D), **i8)
@@ -143,20 +146,23 @@ class LLEPLayer:
         if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
             raise ValueError("the experts do not fit this layer")
         self.gate_up_device = None
-        B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
+        if x_scale is None:
+            B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
+            x, x_scale = self.x_q, self.x_scale
         self.plan(ids, stream)
-        self._permute_int8(ids, gates, stream)
-        B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, self.x_scale,
+        self._permute_int8(ids, gates, x, stream)
+        B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, x_scale,
                                 self.row_pair, experts.gate_up, experts.gate_scale,
                                 experts.up_scale, experts.down, experts.down_scale, self.out_perm,
                                 self.int8_workspace, stream)
         self.combine(gates, stream)
         return self.y
 
-    def _permute_int8(self, ids, gates, stream):
+    def _permute_int8(self, ids, gates, x, stream):
         """The permutation of rows of D bytes, as D / 2 bfloat16."""
         import torch
-        B.llep_permute(self.params, self.bufs, ids, gates, self.x_q.view(torch.bfloat16),
+        B._dense("x", x, (self.T, self.D), torch.int8)
+        B.llep_permute(self.params, self.bufs, ids, gates, x.view(torch.bfloat16),
                        self.x_perm_q.view(torch.bfloat16), self.gate_perm, self.row_pair,
                        self.pair_row, stream)
 
