@@ -393,6 +393,16 @@ def _dense(what: str, t, shape, dtype):
     return t
 
 
+def _all_dense(shape, dtype, tensors) -> bool:
+    """Whether _dense takes all of them (one pass over a call's tensors: a call for one token takes
+    the GPU 4 us)."""
+    for t in tensors:
+        if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_contiguous()
+                                  and t.is_cuda):
+            return False
+    return True
+
+
 def _gate_shape(gate, T: int, D: int, shape) -> int:
     """LLEP_GATE_* of a gate of shape [1, D] or [D], [T, 1], or [T, D] (or None)."""
     if gate is None:
@@ -414,19 +424,21 @@ def llep_block_norm(x, b, gate, w_post, w_pre, alpha: float, eps: float, r, h=No
     [T, D]; gate None, [1, D], [T, 1] or [T, D] (gate_shape: LLEP_GATE_*, where the shape alone
     leaves it open); h_q [T, bytes] int8 with h_scale [T]: h as 8-bit rows. Any of b, gate,
     w_post, w_pre, and outputs, may be None."""
-    import torch
-    T, D = x.shape
+    T, D = size = x.shape
     dt = x.dtype
     code = _dtype_code(x)
     shape = _gate_shape(gate, T, D, gate_shape)
-    for what, t in (("x", x), ("b", b), ("r", r), ("h", h)):
-        _dense(what, t, (T, D), dt)
-    for what, t in (("w_post", w_post), ("w_pre", w_pre)):
-        _dense(what, t, (D,), dt)
+    if not _all_dense(size, dt, (x, b, r, h)):
+        for what, t in (("x", x), ("b", b), ("r", r), ("h", h)):
+            _dense(what, t, (T, D), dt)
+    if not _all_dense((D,), dt, (w_post, w_pre)):
+        for what, t in (("w_post", w_post), ("w_pre", w_pre)):
+            _dense(what, t, (D,), dt)
     if gate is not None:
         _dense("gate", gate, gate.shape, dt)
     q_bytes = 0
     if h_q is not None:
+        import torch
         q_bytes = h_q.shape[-1]
         _dense("h_q", h_q, (T, q_bytes), torch.int8)
         _dense("h_scale", h_scale, (T,), torch.float32)
@@ -445,16 +457,19 @@ def llep_block_norm_backward(r, b, gate, w_post, w_pre, alpha: float, eps: float
     """Every gradient of llep_block_norm (see llep.h): dx, db in x's type; d_gate (the gate's
     shape), dw_post, dw_pre float32; None for inputs that the forward had not."""
     import torch
-    T, D = d_r.shape
+    T, D = size = d_r.shape
     dt = d_r.dtype
     code = _dtype_code(d_r)
     shape = _gate_shape(gate, T, D, gate_shape)
-    for what, t in (("r", r), ("b", b), ("d_r", d_r), ("d_h", d_h), ("dx", dx), ("db", db)):
-        _dense(what, t, (T, D), dt)
-    for what, t in (("w_post", w_post), ("w_pre", w_pre)):
-        _dense(what, t, (D,), dt)
-    for what, t in (("dw_post", dw_post), ("dw_pre", dw_pre)):
-        _dense(what, t, (D,), torch.float32)
+    if not _all_dense(size, dt, (r, b, d_r, d_h, dx, db)):
+        for what, t in (("r", r), ("b", b), ("d_r", d_r), ("d_h", d_h), ("dx", dx), ("db", db)):
+            _dense(what, t, (T, D), dt)
+    if not _all_dense((D,), dt, (w_post, w_pre)):
+        for what, t in (("w_post", w_post), ("w_pre", w_pre)):
+            _dense(what, t, (D,), dt)
+    if not _all_dense((D,), torch.float32, (dw_post, dw_pre)):
+        for what, t in (("dw_post", dw_post), ("dw_pre", dw_pre)):
+            _dense(what, t, (D,), torch.float32)
     if gate is not None:
         _dense("gate", gate, gate.shape, dt)
         _dense("d_gate", d_gate, gate.shape, torch.float32)
