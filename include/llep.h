@@ -504,6 +504,25 @@ int llep_grouped_ffn_int8(const llep_plan_params *params,
                           int32_t D, int32_t F, void *out_perm, void *workspace,
                           size_t workspace_bytes, hipStream_t stream);
 
+/* The same with out_perm [T*K][D] in float32, not rounded to fewer bits, for
+ * llep_combine_to_bf16: the layer's outputs are then rounded once. */
+int llep_grouped_ffn_int8_f32(const llep_plan_params *params,
+                              const llep_plan_buffers *plan, int32_t device,
+                              const int8_t *x_perm, const float *x_scale,
+                              const int32_t *row_pair,
+                              const int8_t *w_gate_up_packed,
+                              const float *gate_scale, const float *up_scale,
+                              const int8_t *w_down_packed,
+                              const float *down_scale, int32_t D, int32_t F,
+                              float *out_perm, void *workspace,
+                              size_t workspace_bytes, hipStream_t stream);
+
+/* llep_combine of float32 rows, y [T][D] rounded once to bfloat16.
+ * Errors: LLEP_E_ARG. */
+int llep_combine_to_bf16(const llep_plan_params *params, const float *out_perm,
+                         const int32_t *pair_row, const float *topk_gates,
+                         int32_t D, void *y, hipStream_t stream);
+
 /* One tensor of a list of gradients: n elements in dtype, dense. `data` and
  * `out` are device pointers; the array of descriptors is host memory, read
  * during the call only. */

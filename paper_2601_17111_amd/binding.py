@@ -46,6 +46,7 @@ EXPORTED = [
     "llep_int8_row_bytes", "llep_quantize_rows", "llep_packed_int8_bytes", "llep_pack_int8",
     "llep_int8_matmul_workspace_bytes", "llep_int8_matmul",
     "llep_grouped_ffn_int8_workspace_bytes", "llep_grouped_ffn_int8",
+    "llep_grouped_ffn_int8_f32", "llep_combine_to_bf16",
 ]
 LLEP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -145,6 +146,9 @@ def lib() -> ctypes.CDLL:
             "llep_grouped_ffn_int8_workspace_bytes": (sz, [pp, i32]),
             "llep_grouped_ffn_int8": (ctypes.c_int, [pp, pb, i32, _P, _P, _P, _P, _P, _P, _P, _P,
                                                      i32, i32, _P, _P, sz, _P]),
+            "llep_grouped_ffn_int8_f32": (ctypes.c_int, [pp, pb, i32, _P, _P, _P, _P, _P, _P, _P,
+                                                         _P, i32, i32, _P, _P, sz, _P]),
+            "llep_combine_to_bf16": (ctypes.c_int, [pp, _P, _P, _P, i32, _P, _P]),
             "llep_clip_gradients_workspace_bytes": (sz, []),
             "llep_gradient_norm": (ctypes.c_int, [i32, pg, _P, _P, sz, _P]),
             "llep_clip_gradients": (ctypes.c_int, [i32, pg, f32, _P, _P, sz, _P]),
@@ -603,7 +607,8 @@ def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: i
                           out_perm, workspace, stream=None):
     """The grouped FFN on 8-bit rows and weights (see llep.h): x_perm [T*K, D] int8, x_scale [T]
     with row_pair [T*K] int32, or [T*K] with row_pair None; weights from llep_pack_matrix_int8,
-    scales [E, F], [E, F] and [E, D]; out_perm [T*K, D] bf16."""
+    scales [E, F], [E, F] and [E, D]; out_perm [T*K, D] bf16, or float32
+    (llep_grouped_ffn_int8_f32)."""
     import torch
     R = params.T * params.K
     D, F, E = x_perm.shape[-1], gate_scale.shape[-1], params.E
@@ -622,9 +627,24 @@ def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: i
         _dense(what, t, (E, n), torch.float32)
     _dense("w_gate_up", w_gate_up, (E, 2 * F * D), torch.int8)
     _dense("w_down", w_down, (E, D * F), torch.int8)
-    _dense("out_perm", out_perm, (out_perm.shape[0], D), torch.bfloat16)
-    _check(lib().llep_grouped_ffn_int8(
+    wide = out_perm.dtype is torch.float32
+    _dense("out_perm", out_perm, (out_perm.shape[0], D), torch.float32 if wide else torch.bfloat16)
+    name = "llep_grouped_ffn_int8_f32" if wide else "llep_grouped_ffn_int8"
+    _check(getattr(lib(), name)(
         ctypes.byref(params), ctypes.byref(bufs.struct), device, _ptr(x_perm), _ptr(x_scale),
         _ptr(row_pair), _ptr(w_gate_up), _ptr(gate_scale), _ptr(up_scale), _ptr(w_down),
         _ptr(down_scale), D, F, _ptr(out_perm), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)), "llep_grouped_ffn_int8")
+        workspace.numel() * workspace.element_size(), _stream(stream)), name)
+
+
+def llep_combine_to_bf16(params: llep_plan_params, out_perm, pair_row, topk_gates, y, stream=None):
+    """llep_combine of float32 rows out_perm [T*K, D] into y [T, D] bf16."""
+    import torch
+    D = out_perm.shape[-1]
+    _dense("out_perm", out_perm, (out_perm.shape[0], D), torch.float32)
+    _dense("y", y, (params.T, D), torch.bfloat16)
+    if out_perm.shape[0] < params.T * params.K:
+        raise ValueError("out_perm needs T * K rows")
+    _check(lib().llep_combine_to_bf16(ctypes.byref(params), _ptr(out_perm), _ptr(pair_row),
+                                      _ptr(topk_gates), D, _ptr(y), _stream(stream)),
+           "llep_combine_to_bf16")

@@ -308,9 +308,9 @@ int llep_grouped_ffn_noalloc(const llep_plan_params *params, const llep_plan_buf
                      "llep_grouped_ffn_noalloc");
 }
 
-int llep_combine(const llep_plan_params *params, const void *out_perm, const int32_t *pair_row,
-                 const float *topk_gates, int32_t D, llep_dtype dtype, void *y,
-                 hipStream_t stream) {
+static int combine(const llep_plan_params *params, const void *out_perm, const int32_t *pair_row,
+                   const float *topk_gates, int32_t D, llep_dtype dtype, void *y, bool bf16_y,
+                   hipStream_t stream, const char *name) {
   int rc = check_params(params);
   if (rc != LLEP_OK) return rc;
   if ((rc = check_rows(D, dtype)) != LLEP_OK) return rc;
@@ -318,7 +318,8 @@ int llep_combine(const llep_plan_params *params, const void *out_perm, const int
   if (params->T > 0 && (!out_perm || !pair_row || !y))
     return fail(LLEP_E_ARG, "a data pointer is null");
   if (!aligned16(out_perm) || !aligned16(y)) return fail(LLEP_E_ARG, "out_perm / y not 16-byte aligned");
-  llep::CombineArgs a;
+  llep::CombineArgs a = {};
+  a.bf16_y = bf16_y;
   a.T = params->T;
   a.K = params->K;
   a.D = D;
@@ -327,7 +328,21 @@ int llep_combine(const llep_plan_params *params, const void *out_perm, const int
   a.pair_row = pair_row;
   a.gates = topk_gates;
   a.y = y;
-  return hip_result(llep::launch_combine(a, stream), "llep_combine");
+  return hip_result(llep::launch_combine(a, stream), name);
+}
+
+int llep_combine(const llep_plan_params *params, const void *out_perm, const int32_t *pair_row,
+                 const float *topk_gates, int32_t D, llep_dtype dtype, void *y,
+                 hipStream_t stream) {
+  return combine(params, out_perm, pair_row, topk_gates, D, dtype, y, false, stream,
+                 "llep_combine");
+}
+
+int llep_combine_to_bf16(const llep_plan_params *params, const float *out_perm,
+                         const int32_t *pair_row, const float *topk_gates, int32_t D, void *y,
+                         hipStream_t stream) {
+  return combine(params, out_perm, pair_row, topk_gates, D, LLEP_F32, y, true, stream,
+                 "llep_combine_to_bf16");
 }
 
 int llep_combine_backward(const llep_plan_params *params, const void *out_perm,
@@ -650,13 +665,13 @@ size_t llep_grouped_ffn_int8_workspace_bytes(const llep_plan_params *params, int
   return llep::ffn_int8_workspace_bytes(params->T * params->K, params->E, params->P, F);
 }
 
-int llep_grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buffers *plan,
-                          int32_t device, const int8_t *x_perm, const float *x_scale,
-                          const int32_t *row_pair, const int8_t *w_gate_up_packed,
-                          const float *gate_scale, const float *up_scale,
-                          const int8_t *w_down_packed, const float *down_scale, int32_t D,
-                          int32_t F, void *out_perm, void *workspace, size_t workspace_bytes,
-                          hipStream_t stream) {
+static int grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buffers *plan,
+                            int32_t device, const int8_t *x_perm, const float *x_scale,
+                            const int32_t *row_pair, const int8_t *w_gate_up_packed,
+                            const float *gate_scale, const float *up_scale,
+                            const int8_t *w_down_packed, const float *down_scale, int32_t D,
+                            int32_t F, void *out_perm, bool f32_out, void *workspace,
+                            size_t workspace_bytes, hipStream_t stream, const char *name) {
   int rc = check_params(params);
   if (rc != LLEP_OK) return rc;
   if ((rc = check_plan_buffers(plan)) != LLEP_OK) return rc;
@@ -693,8 +708,33 @@ int llep_grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buffer
   a.up_scale = up_scale;
   a.down_scale = down_scale;
   a.out_perm = out_perm;
+  a.f32_out = f32_out;
   a.ws = workspace;
-  return hip_result(llep::launch_ffn_int8(a, stream), "llep_grouped_ffn_int8");
+  return hip_result(llep::launch_ffn_int8(a, stream), name);
+}
+
+int llep_grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buffers *plan,
+                          int32_t device, const int8_t *x_perm, const float *x_scale,
+                          const int32_t *row_pair, const int8_t *w_gate_up_packed,
+                          const float *gate_scale, const float *up_scale,
+                          const int8_t *w_down_packed, const float *down_scale, int32_t D,
+                          int32_t F, void *out_perm, void *workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  return grouped_ffn_int8(params, plan, device, x_perm, x_scale, row_pair, w_gate_up_packed,
+                          gate_scale, up_scale, w_down_packed, down_scale, D, F, out_perm, false,
+                          workspace, workspace_bytes, stream, "llep_grouped_ffn_int8");
+}
+
+int llep_grouped_ffn_int8_f32(const llep_plan_params *params, const llep_plan_buffers *plan,
+                              int32_t device, const int8_t *x_perm, const float *x_scale,
+                              const int32_t *row_pair, const int8_t *w_gate_up_packed,
+                              const float *gate_scale, const float *up_scale,
+                              const int8_t *w_down_packed, const float *down_scale, int32_t D,
+                              int32_t F, float *out_perm, void *workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
+  return grouped_ffn_int8(params, plan, device, x_perm, x_scale, row_pair, w_gate_up_packed,
+                          gate_scale, up_scale, w_down_packed, down_scale, D, F, out_perm, true,
+                          workspace, workspace_bytes, stream, "llep_grouped_ffn_int8_f32");
 }
 
 }  // extern "C"

@@ -61,7 +61,8 @@ enum Epilogue : int {
   kEpiSwiglu = 1,
   kEpiSwigluBwd = 2,
   kEpiInt8 = 3,
-  kEpiInt8Swiglu = 4
+  kEpiInt8Swiglu = 4,
+  kEpiInt8F32 = 5
 };
 
 struct GemmArgs {
@@ -88,7 +89,8 @@ struct GemmArgs {
   uint16_t *act;
 };
 
-// 8-bit GEMMs (kEpiInt8, kEpiInt8Swiglu): operands of signed bytes. A byte
+// 8-bit GEMMs (kEpiInt8, kEpiInt8Swiglu, kEpiInt8F32: float32 C of a multiple
+// of 32 columns): operands of signed bytes. A byte
 // matrix is handled as one of half as many 2-byte elements: A, lda, B,
 // b_expert_stride and Kdim above count pairs of bytes, and a 32-deep slice
 // holds 64 bytes of k, which the matrix cores take in two steps of 32.
@@ -360,7 +362,7 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
   constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N;
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr bool kSwiglu = kEpi == kEpiSwiglu;
-  constexpr bool kInt8 = kEpi == kEpiInt8 || kEpi == kEpiInt8Swiglu;
+  constexpr bool kInt8 = kEpi == kEpiInt8 || kEpi == kEpiInt8Swiglu || kEpi == kEpiInt8F32;
   using Frag = std::conditional_t<kInt8, i32x4, bf16x8>;  // 16 bytes of a row along k
   using Acc = std::conditional_t<kInt8, i32x16, f32x16>;
   // DMA blocks (16 rows each) per stage, dealt round-robin over the waves:
@@ -952,6 +954,43 @@ __device__ __forceinline__ void gemm_tiles(const Args g, char *smem, TileCoord t
             const f32x4 v = *reinterpret_cast<const f32x4 *>(stg + row * RS + (lane & 7) * 16);
             if (i * 32 + row < rows_w)
               *reinterpret_cast<f32x4 *>(act + (row0 + row) * F + f + (lane & 7) * 4) = v;
+          }
+        }
+      }
+    } else if constexpr (kEpi == kEpiInt8F32) {
+      // as the SwiGLU epilogue, of one product
+      constexpr int RS = 128 + 16;
+      static_assert(32 * RS + WN * 4 <= STAGING, "staging");
+      float *out = reinterpret_cast<float *>(g.C);
+      float *cols = reinterpret_cast<float *>(stg + 32 * RS);
+#pragma unroll
+      for (int j = 0; j < WN / 64; ++j) cols[j * 64 + lane] = s_col[j];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int col0 = c.n0 + wn * WN + j * 32;
+        if (col0 >= g.N) continue;
+        f32x4 sb[4];
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq)
+          sb[gq] = *reinterpret_cast<const f32x4 *>(cols + j * 32 + 8 * gq + 4 * h);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if (i * 32 >= rows_w) break;
+          const int64_t row0 = int64_t(c.row0) + c.m0 + wm * WM + i * 32;
+          const float sa = __shfl(s_row[i / 2], (i & 1) * 32 + (lane & 31));
+#pragma unroll
+          for (int gq = 0; gq < 4; ++gq) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = int8_value(acc[i][j][4 * gq + e], sa, sb[gq][e]);
+            *reinterpret_cast<f32x4 *>(stg + (lane & 31) * RS + (8 * gq + 4 * h) * 4) = v;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int row = 8 * q + (lane >> 3);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(stg + row * RS + (lane & 7) * 16);
+            if (i * 32 + row < rows_w)
+              *reinterpret_cast<f32x4 *>(out + (row0 + row) * g.ldc + col0 + (lane & 7) * 4) = v;
           }
         }
       }

@@ -675,7 +675,11 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   d.row_pair = nullptr;
   d.b_scale = a.down_scale;
   d.scale_stride = a.D;
+  d.f32_out = a.f32_out;
   if (streams) return launch_int8_stream<true, false>(d, rows, mt_most, bytes, stream);
+  if (a.f32_out)
+    return rows == 128 ? run_int8_tiles<128, 128, 2, 2, kEpiInt8F32, true>(d, stream)
+                       : run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8F32, true>(d, stream);
   if (rows == 128) return run_int8_tiles<128, 128, 2, 2, kEpiInt8, true>(d, stream);
   return run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8, true>(d, stream);
 }

@@ -60,6 +60,7 @@ struct CombineArgs {
   const int32_t *pair_row;
   const float *gates;
   void *y;
+  bool bf16_y;  // float32 out_perm: whether y is bfloat16 all the same
 };
 hipError_t launch_combine(const CombineArgs &a, hipStream_t stream);
 
@@ -179,6 +180,7 @@ struct FfnInt8Args {
   const int8_t *x_perm, *w_gate_up, *w_down;
   const float *x_scale, *gate_scale, *up_scale, *down_scale;
   void *out_perm, *ws;
+  bool f32_out;  // out_perm is float32, else bfloat16
 };
 size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F);
 hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream);

@@ -411,8 +411,8 @@ hipError_t launch_permute(const PermuteArgs &a, hipStream_t stream) {
 // One wavefront per (token, slice of kV * 64 vectors of the output row);
 // the pairs' rows are read kCombinePairs at a time with all their loads in
 // flight before they are summed (in k order, so the result does not depend
-// on the slicing).
-template <bool kBf16, int kV>
+// on the slicing). kNarrow: y in bfloat16 from float32 rows.
+template <bool kBf16, int kV, bool kNarrow = false>
 __global__ __launch_bounds__(256) void combine_kernel(const i32x4 *__restrict__ out_perm,
                                                       const int32_t *__restrict__ pair_row,
                                                       const float *__restrict__ gates,
@@ -480,6 +480,16 @@ __global__ __launch_bounds__(256) void combine_kernel(const i32x4 *__restrict__ 
           }
         }
       }
+      if constexpr (kNarrow) {
+        uint2 *dst = reinterpret_cast<uint2 *>(y) + t * vecs;
+#pragma unroll
+        for (int b = 0; b < kV; ++b) {
+          const int v = v0 + b * kWave + lane;
+          if (v < vecs)
+            dst[v] = make_uint2(pack_bf16x2(acc[b][0], acc[b][1]), pack_bf16x2(acc[b][2], acc[b][3]));
+        }
+        continue;
+      }
       i32x4 *dst = y + t * vecs;
 #pragma unroll
       for (int b = 0; b < kV; ++b) {
@@ -501,23 +511,23 @@ __global__ __launch_bounds__(256) void combine_kernel(const i32x4 *__restrict__ 
   }
 }
 
-template <bool kBf16, int kV>
+template <bool kBf16, int kV, bool kNarrow>
 void launch_combine_v(int grid, hipStream_t stream, const CombineArgs &a, int32_t vecs) {
-  hipLaunchKernelGGL((combine_kernel<kBf16, kV>), dim3(grid), dim3(256), 0, stream,
+  hipLaunchKernelGGL((combine_kernel<kBf16, kV, kNarrow>), dim3(grid), dim3(256), 0, stream,
                      static_cast<const i32x4 *>(a.out_perm), a.pair_row, a.gates,
                      static_cast<i32x4 *>(a.y), a.T, a.K, vecs);
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kNarrow = false>
 void launch_combine_t(hipStream_t stream, const CombineArgs &a, int32_t vecs) {
   const int kv = vecs_per_lane(vecs, kCombineMaxVecs);
   const int64_t blocks = (a.T * ((vecs + kv * kWave - 1) / (kv * kWave)) + 3) / 4;
   const int grid = int(blocks < 65536 ? blocks : 65536);
   switch (kv) {
-    case 1: launch_combine_v<kBf16, 1>(grid, stream, a, vecs); break;
-    case 2: launch_combine_v<kBf16, 2>(grid, stream, a, vecs); break;
-    case 3: launch_combine_v<kBf16, 3>(grid, stream, a, vecs); break;
-    default: launch_combine_v<kBf16, 4>(grid, stream, a, vecs); break;
+    case 1: launch_combine_v<kBf16, 1, kNarrow>(grid, stream, a, vecs); break;
+    case 2: launch_combine_v<kBf16, 2, kNarrow>(grid, stream, a, vecs); break;
+    case 3: launch_combine_v<kBf16, 3, kNarrow>(grid, stream, a, vecs); break;
+    default: launch_combine_v<kBf16, 4, kNarrow>(grid, stream, a, vecs); break;
   }
 }
 
@@ -527,6 +537,8 @@ hipError_t launch_combine(const CombineArgs &a, hipStream_t stream) {
   const int32_t vecs = int32_t((int64_t(a.D) * eb) / 16);
   if (a.dtype == LLEP_BF16)
     launch_combine_t<true>(stream, a, vecs);
+  else if (a.bf16_y)
+    launch_combine_t<false, true>(stream, a, vecs);
   else
     launch_combine_t<false>(stream, a, vecs);
   return hipGetLastError();

@@ -274,6 +274,41 @@ def test_grouped_ffn_sizes_of_calls_agree(dev):
         assert torch.equal(got, whole[[of[int(p)] for p in S["row_pair"]]]), t
 
 
+@pytest.mark.parametrize("T,K,E,P,D,F,hot", [
+    (1, 4, 8, 4, 128, 192, 0.0), (20, 4, 16, 4, 256, 320, 0.7), (130, 2, 16, 4, 192, 256, 0.6),
+    (300, 4, 8, 4, 128, 192, 0.6), (700, 2, 4, 2, 576, 320, 0.8), (1100, 1, 2, 1, 64, 64, 0.5),
+    (2100, 2, 4, 2, 320, 1088, 0.5),
+])
+def test_grouped_ffn_float32_outputs(dev, T, K, E, P, D, F, hot):
+    """Float32 outputs are the values that the bfloat16 ones are rounded from, and
+    llep_combine_to_bf16 sums them with one rounding (float32 sums of K products:
+    K 2^-23 of their magnitudes)."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    L = _layer(dev, T, K, E, P, D, F, hot, 3 * T + E)
+    narrow = _ffn(L, -1)
+    e = L["experts"]
+    tok = L["row_pair"] // K
+    wide = torch.full((T * K, D), float("nan"), device=dev)
+    ws = torch.empty(B.llep_grouped_ffn_int8_workspace_bytes(L["params"], F), dtype=torch.uint8,
+                     device=dev)
+    B.llep_grouped_ffn_int8(L["params"], L["bufs"], -1, torch.from_numpy(L["x"][tok]).to(dev),
+                            torch.from_numpy(L["s"]).to(dev),
+                            torch.from_numpy(L["row_pair"].astype(np.int32)).to(dev), e.gate_up,
+                            e.gate_scale, e.up_scale, e.down, e.down_scale, wide, ws)
+    gates = np.random.default_rng(T).uniform(0, 1, (T, K)).astype(np.float32)
+    pair_row = torch.from_numpy(np.asarray(L["pair_row"], dtype=np.int32)).to(dev)
+    y = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+    B.llep_combine_to_bf16(L["params"], wide, pair_row, torch.from_numpy(gates).to(dev), y)
+    torch.cuda.synchronize()
+    assert torch.equal(wide.bfloat16(), narrow)
+    rows = wide.double().cpu().numpy()[np.asarray(L["pair_row"])].reshape(T, K, D)
+    terms = rows * gates[:, :, None]
+    want = terms.sum(1)
+    tol = 2.0 ** -8 * np.abs(want) + K * 2.0 ** -23 * np.abs(terms).sum(1)
+    assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
+
+
 @pytest.mark.parametrize("T,hot", [(1, 0.0), (37, 0.5), (600, 0.7)])
 def test_layer_near_the_bf16_layer(dev, T, hot):
     """LLEPLayer.forward_int8 with experts from bf16 weights: near forward(), as
