@@ -507,7 +507,11 @@ hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t st
 }
 
 // The stream for `mtiles` row tiles (at most) of at most `rows` rows: 16, 32 or
-// 64. Up to 16 rows, with few weights, k is split over more wavefronts, so that
+// 64. With up to 256 units of 64 x 64 outputs k is split over eight wavefronts
+// (4 / 8: 64 x 7168 x 2048 7.0 / 6.5 us, 32 x 7168 x 7168 15.7 / 12.9, but 333 x
+// 2880 x 1024, 270 units, 7.5 / 9.3); with many of them a workgroup takes 64 x
+// 128 outputs, with fewer bytes from the L2 per product (2048^3 26 / 22 us, 512 x
+// 7168 x 2048 21 / 18). Up to 16 rows, with few weights, k is split over more wavefronts, so that
 // about 1024 are at work (1 row, N x K = 7168 x 2048 with 4 / 8 / 16
 // wavefronts: 5.6 / 3.8 / 4.7 us; 768 x 7168: 9.4 / - / 4.9 us).
 // bytes: of all weights that the call reads. Beyond half of the 256 MB cache
@@ -518,9 +522,16 @@ template <bool kGrouped, bool kSwigluOut>
 hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, int64_t bytes,
                               hipStream_t stream) {
   constexpr bool G = kGrouped, S = kSwigluOut;
-  if (rows > 32) return run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
-  if (rows > 16) return run_int8_stream<2, 4, 4, G, S, false>(g, mtiles, stream);
   const int64_t units = mtiles * ((g.N + 63) / 64);  // of 64 packed rows
+  if (rows > 32) {
+    if constexpr (!G && !S)
+      if (units >= 800) return run_int8_stream<4, 8, 4, G, S, false>(g, mtiles, stream);
+    return units <= 256 ? run_int8_stream<4, 4, 8, G, S, false>(g, mtiles, stream)
+                        : run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
+  }
+  if (rows > 16)
+    return units <= 256 ? run_int8_stream<2, 4, 8, G, S, false>(g, mtiles, stream)
+                        : run_int8_stream<2, 4, 4, G, S, false>(g, mtiles, stream);
   if (units * 4 >= 1024)
     return bytes > (int64_t(128) << 20) ? run_int8_stream<1, 4, 4, G, S, true>(g, mtiles, stream)
                                         : run_int8_stream<1, 4, 4, G, S, false>(g, mtiles, stream);
@@ -550,12 +561,12 @@ hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream) {
   g.M = a.M;
   g.f32_out = a.dtype == LLEP_F32;
   // The ring's 256 x 256 tiles take about 1 us per 64 bytes of k however few
-  // there are, one on each compute unit, the stream 2.9 fs per multiply-add:
-  // 2048^3 40 / 26 us, 512 x 7168 x 2048 35 / 21, 512 x 2048 x 7168 66 / 19,
-  // 4096^3 70 / 105 (tiles / stream).
+  // there are, one on each compute unit, the stream 2.7 fs per multiply-add:
+  // 2048^3 40 / 22 us, 512 x 7168 x 2048 35 / 18, 512 x 2048 x 7168 66 / 18
+  // (tiles / stream).
   const double tiles = double((a.M + 255) / 256) * double((a.N + 255) / 256);
   const double ring = std::ceil(tiles / cu_count()) * (Kp / 64) * 1.0;
-  const double streamed = 2.9e-9 * double(a.M) * double(a.N) * double(a.K);
+  const double streamed = 2.7e-9 * double(a.M) * double(a.N) * double(a.K);
   if (a.M <= 64 || streamed < ring) {
     const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
     return launch_int8_stream<false, false>(g, rows, (a.M + rows - 1) / rows,
