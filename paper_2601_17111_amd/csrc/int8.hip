@@ -227,9 +227,11 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
   // reads 16 rows for an operand touches 16 lines with every quarter of its
   // lanes, four times the work of the same bytes in order.
   constexpr bool kStaged = kMB > 1;
-  // blocks of k requested together, and 16 x 16 blocks of the outputs whose
-  // parts are in LDS at a time
-  constexpr int kUnroll = kStaged ? 1 : 4;
+  // blocks of k requested together (two where all of the chip's wavefronts are
+  // at work: more of them fit; an expert layer of 8 tokens, 15 experts of 2880 x
+  // 2880, 97.5 -> 95.7 us), and 16 x 16 blocks of the outputs whose parts are in
+  // LDS at a time
+  constexpr int kUnroll = kStaged ? 1 : kOnce ? 2 : 4;
   constexpr int kRound = kBlocks >= 16 ? 8 : kBlocks;
   constexpr int kStage = kUnroll * kMB * 1024;  // bytes of A per wavefront, twice
   constexpr int kLdsBytes = kStaged && 2 * kStage > kRound * 1024 ? 2 * kStage : kRound * 1024;
@@ -253,12 +255,14 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
     int e = 0;
     int64_t row0 = int64_t(mt) * 16 * kMB;
     int rows;
+    bool lone = n_mt == 1;  // no other row tile of the same weights
     if (kGrouped) {
       const int4 te = g.tiles[mt];
       const int32_t *gr = g.groups + 4 * te.x;
       e = gr[1];
       row0 = int64_t(gr[2]) + te.y * 16 * kMB;
       rows = min(16 * kMB, gr[3] - te.y * 16 * kMB);
+      lone = __builtin_amdgcn_readfirstlane(gr[3]) <= 16 * kMB;
     } else {
       rows = int(min<int64_t>(16 * kMB, g.M - row0));
     }
@@ -277,103 +281,115 @@ __global__ __launch_bounds__(kWaves * kWave) void int8_stream_kernel(Int8GemmArg
     for (int n = 0; n < kNB; ++n)  // and past the last block
       offB[n] = uint32_t(min(n * kApart, n_blk - 1 - blk0)) * uint32_t(g.b_blk_stride) +
                 lane * 16;
-    // kOnce: weights that no later call finds in a cache pass by them
-    auto load_weights = [](const int8_t *p) {
-      if constexpr (kOnce)
-        return __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(p));
-      else
-        return *reinterpret_cast<const i32x4 *>(p);
-    };
     i32x4 acc[kMB][kNB];
 #pragma unroll
     for (int m = 0; m < kMB; ++m)
 #pragma unroll
       for (int n = 0; n < kNB; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
-    if constexpr (kStaged) {
-      // One step of kUnroll blocks of k ahead: its rows of A on their way to
-      // the wavefront's other half of LDS (lane l: row l / 4 of 16, 16 bytes of
-      // it), its weights to registers; the wait at the top of a step is for
-      // everything, so both are there. No barrier: each wavefront has its own
-      // part of LDS. Blocks past the last one are the last again, not used.
-      const char *stage = lds + wave * kLdsBytes;
-      const uint32_t stage_at = lds_addr(lds) + wave * kLdsBytes;
-      int32_t offS[kMB];
-#pragma unroll
-      for (int m = 0; m < kMB; ++m)
-        offS[m] = min(m * 16 + (lane >> 2), rows - 1) * int32_t(g.lda * 2) +
-                  (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
-      i32x4 fb[kUnroll][kNB];
-      auto request = [&](int kb, int half) {
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int k = min(kb + u, kb1 - 1);
-#pragma unroll
-          for (int m = 0; m < kMB; ++m)
-            dma16(reinterpret_cast<const char *>(A) + k * 64, offS[m],
-                  stage_at + half * kStage + (u * kMB + m) * 1024);
-#pragma unroll
-          for (int n = 0; n < kNB; ++n)
-            fb[u][n] = *reinterpret_cast<const i32x4 *>(B + int64_t(k) * 1024 + offB[n]);
-        }
+    // past: the weights are read past the caches
+    auto product = [&](auto past) {
+      auto load_weights = [](const int8_t *p) {
+        if constexpr (decltype(past)::value)
+          return __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(p));
+        else
+          return *reinterpret_cast<const i32x4 *>(p);
       };
-      if (kb0 < kb1) request(kb0, 0);
-      int half = 0;
-      for (int kb = kb0; kb < kb1; kb += kUnroll) {
+      if constexpr (kStaged) {
+        // One step of kUnroll blocks of k ahead: its rows of A on their way to
+        // the wavefront's other half of LDS (lane l: row l / 4 of 16, 16 bytes of
+        // it), its weights to registers; the wait at the top of a step is for
+        // everything, so both are there. No barrier: each wavefront has its own
+        // part of LDS. Blocks past the last one are the last again, not used.
+        const char *stage = lds + wave * kLdsBytes;
+        const uint32_t stage_at = lds_addr(lds) + wave * kLdsBytes;
+        int32_t offS[kMB];
+#pragma unroll
+        for (int m = 0; m < kMB; ++m)
+          offS[m] = min(m * 16 + (lane >> 2), rows - 1) * int32_t(g.lda * 2) +
+                    (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
+        i32x4 fb[kUnroll][kNB];
+        auto request = [&](int kb, int half) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) {
+            const int k = min(kb + u, kb1 - 1);
+#pragma unroll
+            for (int m = 0; m < kMB; ++m)
+              dma16(reinterpret_cast<const char *>(A) + k * 64, offS[m],
+                    stage_at + half * kStage + (u * kMB + m) * 1024);
+#pragma unroll
+            for (int n = 0; n < kNB; ++n)
+              fb[u][n] = load_weights(B + int64_t(k) * 1024 + offB[n]);
+          }
+        };
+        if (kb0 < kb1) request(kb0, 0);
+        int half = 0;
+        for (int kb = kb0; kb < kb1; kb += kUnroll) {
+          asm volatile("" ::: "memory");
+          wait_cnt<0, 0>();
+          asm volatile("" ::: "memory");
+          i32x4 now[kUnroll][kNB];
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int n = 0; n < kNB; ++n) now[u][n] = fb[u][n];
+          if (kb + kUnroll < kb1) request(kb + kUnroll, half ^ 1);
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) {
+            if (kb + u >= kb1) break;
+#pragma unroll
+            for (int m = 0; m < kMB; ++m) {
+              const int r = lane & 15;
+              const i32x4 fa = *reinterpret_cast<const i32x4 *>(
+                  stage + half * kStage + (u * kMB + m) * 1024 + r * 64 +
+                  (((lane >> 4) ^ ((r >> 2) & 3)) << 4));
+#pragma unroll
+              for (int n = 0; n < kNB; ++n)
+                acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][n], fa, acc[m][n], 0, 0, 0);
+            }
+          }
+          half ^= 1;
+        }
+        // the parts below go over the stages: every wavefront's reads are done
         asm volatile("" ::: "memory");
         wait_cnt<0, 0>();
-        asm volatile("" ::: "memory");
-        i32x4 now[kUnroll][kNB];
+        __syncthreads();
+      } else {
+        auto steps = [&](auto count, int kb) {
+          constexpr int kU = decltype(count)::value;
+          i32x4 fa[kU][kMB], fb[kU][kNB];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-          for (int n = 0; n < kNB; ++n) now[u][n] = fb[u][n];
-        if (kb + kUnroll < kb1) request(kb + kUnroll, half ^ 1);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          if (kb + u >= kb1) break;
-#pragma unroll
-          for (int m = 0; m < kMB; ++m) {
-            const int r = lane & 15;
-            const i32x4 fa = *reinterpret_cast<const i32x4 *>(
-                stage + half * kStage + (u * kMB + m) * 1024 + r * 64 +
-                (((lane >> 4) ^ ((r >> 2) & 3)) << 4));
+          for (int u = 0; u < kU; ++u) {
 #pragma unroll
             for (int n = 0; n < kNB; ++n)
-              acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][n], fa, acc[m][n], 0, 0, 0);
+              fb[u][n] = load_weights(B + int64_t(kb + u) * 1024 + offB[n]);
+#pragma unroll
+            for (int m = 0; m < kMB; ++m)
+              fa[u][m] = *reinterpret_cast<const i32x4 *>(A + (kb + u) * 64 + offA[m]);
           }
+#pragma unroll
+          for (int u = 0; u < kU; ++u)
+#pragma unroll
+            for (int m = 0; m < kMB; ++m)
+#pragma unroll
+              for (int n = 0; n < kNB; ++n)
+                acc[m][n] =
+                    __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][n], fa[u][m], acc[m][n], 0, 0, 0);
+        };
+        int kb = kb0;
+        for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
+        // the rest together: one wait, not one for each
+        switch (kb1 - kb) {
+          case 3: steps(std::integral_constant<int, 3>{}, kb); break;
+          case 2: steps(std::integral_constant<int, 2>{}, kb); break;
+          case 1: steps(std::integral_constant<int, 1>{}, kb); break;
+          default: break;
         }
-        half ^= 1;
       }
-      // the parts below go over the stages: every wavefront's reads are done
-      asm volatile("" ::: "memory");
-      wait_cnt<0, 0>();
-      __syncthreads();
-    } else {
-      auto steps = [&](auto count, int kb) {
-        constexpr int kU = decltype(count)::value;
-        i32x4 fa[kU][kMB], fb[kU][kNB];
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-#pragma unroll
-          for (int n = 0; n < kNB; ++n)
-            fb[u][n] = load_weights(B + int64_t(kb + u) * 1024 + offB[n]);
-#pragma unroll
-          for (int m = 0; m < kMB; ++m)
-            fa[u][m] = *reinterpret_cast<const i32x4 *>(A + (kb + u) * 64 + offA[m]);
-        }
-#pragma unroll
-        for (int u = 0; u < kU; ++u)
-#pragma unroll
-          for (int m = 0; m < kMB; ++m)
-#pragma unroll
-            for (int n = 0; n < kNB; ++n)
-              acc[m][n] =
-                  __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][n], fa[u][m], acc[m][n], 0, 0, 0);
-      };
-      int kb = kb0;
-      for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
-      for (; kb < kb1; ++kb) steps(std::integral_constant<int, 1>{}, kb);
-    }
+    };
+    if (kOnce && lone)
+      product(std::true_type{});
+    else
+      product(std::false_type{});
 #pragma unroll
     for (int b0 = 0; b0 < kBlocks; b0 += kRound) {
 #pragma unroll
@@ -515,9 +531,10 @@ hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t st
 // about 1024 are at work (1 row, N x K = 7168 x 2048 with 4 / 8 / 16
 // wavefronts: 5.6 / 3.8 / 4.7 us; 768 x 7168: 9.4 / - / 4.9 us).
 // bytes: of all weights that the call reads. Beyond half of the 256 MB cache
-// behind the L2s they are read past the caches (16 rows; 15 experts of 2880 x
-// 2880 in use, 376 MB: 105 -> 98 us; 4 experts, 100 MB, the same four in every
-// call: 44 -> 49 us).
+// behind the L2s they are read past the caches, in units of 32 packed rows (16
+// rows; 15 experts of 2880 x 2880 in use, 376 MB: 105 -> 98 us, 96 -> 94 with the
+// smaller units, whose last ones end together; 4 experts, 100 MB, the same four
+// in every call: 44 -> 49 us).
 template <bool kGrouped, bool kSwigluOut>
 hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, int64_t bytes,
                               hipStream_t stream) {
@@ -529,12 +546,14 @@ hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, i
     return units <= 256 ? run_int8_stream<4, 4, 8, G, S, false>(g, mtiles, stream)
                         : run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
   }
+  const bool once = bytes > (int64_t(128) << 20);
+  if (rows > 16 && G && once) return run_int8_stream<2, 4, 4, G, S, G>(g, mtiles, stream);
   if (rows > 16)
     return units <= 256 ? run_int8_stream<2, 4, 8, G, S, false>(g, mtiles, stream)
                         : run_int8_stream<2, 4, 4, G, S, false>(g, mtiles, stream);
   if (units * 4 >= 1024)
-    return bytes > (int64_t(128) << 20) ? run_int8_stream<1, 4, 4, G, S, true>(g, mtiles, stream)
-                                        : run_int8_stream<1, 4, 4, G, S, false>(g, mtiles, stream);
+    return once ? run_int8_stream<1, 2, 4, G, S, true>(g, mtiles, stream)
+                : run_int8_stream<1, 4, 4, G, S, false>(g, mtiles, stream);
   if (S || units * 16 >= 1024) return run_int8_stream<1, 2, 8, G, S, false>(g, mtiles, stream);
   if constexpr (!S) return run_int8_stream<1, 1, 16, G, S, false>(g, mtiles, stream);
   return hipErrorInvalidValue;

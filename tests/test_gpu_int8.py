@@ -309,6 +309,45 @@ def test_grouped_ffn_float32_outputs(dev, T, K, E, P, D, F, hot):
     assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
 
 
+@pytest.mark.parametrize("T,hot", [(2, 0.0), (30, 0.7), (40, 0.6)])
+def test_grouped_ffn_of_large_weights(dev, T, hot):
+    """Weights of more than half the cache, which rows that have them to themselves read past it:
+    row tiles of 16 and of 32 rows, experts of one tile and a hot one of several; 24 rows checked
+    (the tolerance of above: five steps, F = 2048 having about one of them expected)."""
+    import torch
+    L = _layer(dev, T, 4, 16, 4, 2880, 2048, hot, T)
+    R = T * 4
+    assert 3 * min(R, 16) * 2880 * 2048 > 128 << 20
+    out = _ffn(L, -1)
+    assert not torch.isnan(out).any()
+    _check_ffn(L, out, np.unique(np.linspace(0, R - 1, min(R, 24)).astype(int)))
+    assert torch.equal(_ffn(L, -1, by_row=True), out)
+
+
+def test_product_of_a_large_matrix(dev):
+    """A matrix of more than half the cache by a few rows: the same bits as by more rows."""
+    import torch
+    g = torch.Generator(device=dev).manual_seed(4)
+    N, K, M = 70001, 2048, 40
+    w = torch.randint(-127, 128, (N, K), generator=g, device=dev, dtype=torch.int8)
+    q = torch.randint(-127, 128, (M, K), generator=g, device=dev, dtype=torch.int8)
+    s = torch.rand(M, generator=g, device=dev) + 0.5
+    ws = (torch.rand(N, generator=g, device=dev) + 0.5).cpu().numpy()
+    from paper_2601_17111_amd import binding as B
+    packed, wsd = B.llep_pack_matrix_int8(w), torch.from_numpy(ws).to(dev)
+    outs = []
+    for m in (40, 16, 3):
+        out = torch.full((m, N), float("nan"), device=dev)
+        B.llep_int8_matmul(q[:m], s[:m], packed, wsd, out, K)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][:16], outs[1]) and torch.equal(outs[0][:3], outs[2])
+    cols = np.linspace(0, N - 1, 300).astype(int)
+    want = oracle.int8_product(q.cpu().numpy(), s.cpu().numpy(), w.cpu().numpy()[cols], ws[cols])
+    got = outs[0].double().cpu().numpy()[:, cols]
+    assert (np.abs(got - want) <= 2.0 ** -22 * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("T,hot", [(1, 0.0), (37, 0.5), (600, 0.7)])
 def test_layer_near_the_bf16_layer(dev, T, hot):
     """LLEPLayer.forward_int8 with experts from bf16 weights: near forward(), as
