@@ -523,29 +523,31 @@ hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t st
 }
 
 // The stream for `mtiles` row tiles (at most) of at most `rows` rows: 16, 32 or
-// 64. With up to 256 units of 64 x 64 outputs k is split over eight wavefronts
-// (4 / 8: 64 x 7168 x 2048 7.0 / 6.5 us, 32 x 7168 x 7168 15.7 / 12.9, but 333 x
-// 2880 x 1024, 270 units, 7.5 / 9.3); with many of them a workgroup takes 64 x
-// 128 outputs, with fewer bytes from the L2 per product (2048^3 26 / 22 us, 512 x
-// 7168 x 2048 21 / 18). Up to 16 rows, with few weights, k is split over more wavefronts, so that
-// about 1024 are at work (1 row, N x K = 7168 x 2048 with 4 / 8 / 16
-// wavefronts: 5.6 / 3.8 / 4.7 us; 768 x 7168: 9.4 / - / 4.9 us).
-// bytes: of all weights that the call reads. Beyond half of the 256 MB cache
-// behind the L2s they are read past the caches, in units of 32 packed rows (16
-// rows; 15 experts of 2880 x 2880 in use, 376 MB: 105 -> 98 us, 96 -> 94 with the
-// smaller units, whose last ones end together; 4 experts, 100 MB, the same four
-// in every call: 44 -> 49 us).
+// (dense) 64; bytes: of all weights that the call reads.
+// - With up to 256 units of 64 columns k is split over eight wavefronts (4 / 8:
+//   64 x 7168 x 2048 7.0 / 6.5 us, 32 x 7168 x 7168 15.7 / 12.9, but 333 x 2880 x
+//   1024, 270 units, 7.5 / 9.3). With many, a workgroup takes 64 x 128 outputs,
+//   with fewer bytes from the L2 per product (2048^3 26 / 22 us, 512 x 7168 x
+//   2048 21 / 18).
+// - Up to 16 rows, with few weights, k is split so that about 1024 wavefronts
+//   are at work (1 row, N x K = 7168 x 2048 with 4 / 8 / 16: 5.6 / 3.8 / 4.7 us;
+//   768 x 7168: 9.4 / - / 4.9 us).
+// - Weights of more than half of the 256 MB cache behind the L2s are read past
+//   the caches by row tiles that have them to themselves, and for 16 rows in
+//   units of 32 packed rows, whose last ones end together (15 experts of 2880 x
+//   2880 in use, 376 MB: 105 -> 98 -> 94 us; 32 rows, 32 such experts 195 -> 174;
+//   but 4 of them, 100 MB, the same four in every call: 44 -> 49 us).
 template <bool kGrouped, bool kSwigluOut>
 hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, int64_t bytes,
                               hipStream_t stream) {
   constexpr bool G = kGrouped, S = kSwigluOut;
   const int64_t units = mtiles * ((g.N + 63) / 64);  // of 64 packed rows
-  if (rows > 32) {
-    if constexpr (!G && !S)
+  if constexpr (!G)
+    if (rows > 32) {
       if (units >= 800) return run_int8_stream<4, 8, 4, G, S, false>(g, mtiles, stream);
-    return units <= 256 ? run_int8_stream<4, 4, 8, G, S, false>(g, mtiles, stream)
-                        : run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
-  }
+      return units <= 256 ? run_int8_stream<4, 4, 8, G, S, false>(g, mtiles, stream)
+                          : run_int8_stream<4, 4, 4, G, S, false>(g, mtiles, stream);
+    }
   const bool once = bytes > (int64_t(128) << 20);
   if (rows > 16 && G && once) return run_int8_stream<2, 4, 4, G, S, G>(g, mtiles, stream);
   if (rows > 16)
@@ -557,10 +559,6 @@ hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, i
   if (S || units * 16 >= 1024) return run_int8_stream<1, 2, 8, G, S, false>(g, mtiles, stream);
   if constexpr (!S) return run_int8_stream<1, 1, 16, G, S, false>(g, mtiles, stream);
   return hipErrorInvalidValue;
-}
-
-size_t int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K) {
-  return 0;
 }
 
 hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream) {
@@ -616,26 +614,27 @@ size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F) {
 }
 
 // Rows of a tile, by the rows per expert on average (the routing is not known
-// here): the stream's 16, 32 or 64, or 128 or 256 rows through the ring. Whole
-// layers in us with 16 / 32 / 64 / 128 / 256 rows, uniform routing:
-//   2880 x 2880, 32 experts, 4 of them a token:
-//     32 tokens 176 / 177 / 182 / 189 / 184, 128 tokens 218 / 193 / 194 / 200 / 201,
-//     300 tokens 352 / 267 / 230 / 226 / 217, 700 tokens 685 / 403 / 344 / 269 / 254
-//   2048 x 768, 128 experts, 8: 128 tokens 149 / 149 / 159 / 167 / 178,
-//     700 tokens 236 / 209 / 197 / 195 / 196, 1500 tokens 378 / 290 / 279 / 220 / 239,
-//     3000 tokens 808 / 458 / 421 / 340 / 302
-//   1024 x 768, 16 experts, 2: 300 tokens 53 / 48 / 48 / 60 / 67,
-//     1500 tokens 75 / 64 / 63 / 64 / 80, 3000 tokens 116 / 95 / 92 / 85 / 88
-// (60% of the pairs on four experts: the same order, closer together.)
+// here): the stream's 16 or 32, or 128 or 256 rows through the ring. Whole
+// layers in us, uniform routing unless "hot" (60% of the pairs on four experts):
+//   2880 x 2880, 32 experts, 4 of them a token, 16 / 32 / 128 / 256 rows:
+//     32 tokens 176 / 177 / 189 / 184, 128 tokens 218 / 193 / 200 / 201,
+//     and 32 / 128 / 256: 250 tokens 242 / 210 / 223, 400 tokens 299 / 227 / 220,
+//     hot 272 / 252 / 245, 1000 tokens hot 541 / 316 / 289
+//   2048 x 768, 128 experts, 8, 32 / 128 / 256 rows: 400 tokens 157 / 158 / 162,
+//     700 tokens 209 / 175 / 177, 1531 tokens 293 / 204 / 207,
+//     2200 tokens hot 370 / 263 / 269, 3000 tokens 452 / 305 / 266
+//   1024 x 768, 16 experts, 2: 300 tokens 42 / 50 / 51, 700 tokens 49 / 56 / 58,
+//     1200 tokens hot 62 / 59 / 69, 2000 tokens 75 / 61 / 72
 static int ffn_int8_rows(const FfnInt8Args &a) {
-  const int64_t R = a.R, E = a.E;
+  const int64_t R = a.R, E = a.E, weight = int64_t(a.D) * a.F;
   if (R <= 8 * E) return 16;
-  if (R <= 24 * E) return 32;
-  const int64_t weight = int64_t(a.D) * a.F;
-  if (weight * R <= int64_t(3000000000)) return 64;
-  // 128 rows where 256 would be half empty, or too few tiles for the chip
+  // up to 24 rows an expert the weights are most of the work; small layers have
+  // too few tiles for the chip
+  if (R <= 24 * E || weight * R <= int64_t(1500000000)) return 32;
+  // 256 rows where most would be valid (long products: fewer), and a few rounds
+  // of such tiles
   const int64_t tiles = (R / 256 + E) * ((a.F + 127) / 128);
-  return (R <= 128 * E && weight <= 2000000) || tiles < 256 ? 128 : 256;
+  return (R > 128 * E || (weight > 2000000 && R > 40 * E)) && tiles >= 512 ? 256 : 128;
 }
 
 hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
@@ -648,7 +647,7 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   int8_t *act_q = reinterpret_cast<int8_t *>(ws + w.act_q);
   float *act_scale = reinterpret_cast<float *>(ws + w.scale);
   const int rows = ffn_int8_rows(a);
-  const bool streams = rows <= 64;
+  const bool streams = rows <= 32;
   const int64_t bytes = 3 * std::min<int64_t>(a.R, a.E) * a.D * a.F;  // of the weights, at most
   hipError_t err = launch_tile_table(a.groups, a.group_begin, 2 * a.E + a.P, a.device, a.P, rows,
                                      tiles, n_mtiles, stream);

@@ -169,9 +169,8 @@ struct Int8MatmulArgs {
   llep_dtype dtype;  // of out
   const int8_t *x, *w;
   const float *x_scale, *w_scale;
-  void *out, *ws;
+  void *out;
 };
-size_t int8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K);
 hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream);
 struct FfnInt8Args {
   int64_t R;
