@@ -407,11 +407,27 @@ def _all_dense(shape, dtype, tensors) -> bool:
     return True
 
 
+def _workspace(ws):
+    """Pointer and bytes of a dense GPU tensor used as a workspace (or None)."""
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous() or not ws.is_cuda:
+        raise ValueError("the workspace is not a contiguous GPU tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _gate_shape(gate, T: int, D: int, shape) -> int:
-    """LLEP_GATE_* of a gate of shape [1, D] or [D], [T, 1], or [T, D] (or None)."""
+    """LLEP_GATE_* of a gate of shape [1, D] or [D], [T, 1], or [T, D] (or None); `shape`, where
+    given, has to fit it."""
     if gate is None:
+        if shape is not None and shape != LLEP_GATE_NONE and T > 0:
+            raise ValueError("gate_shape without a gate")
         return LLEP_GATE_NONE
     if shape is not None:
+        fits = {LLEP_GATE_CHANNEL: ((1, D), (D,)), LLEP_GATE_TOKEN: ((T, 1),),
+                LLEP_GATE_FULL: ((T, D),)}.get(shape, ())
+        if tuple(gate.shape) not in fits:
+            raise ValueError(f"gate of shape {tuple(gate.shape)} does not fit gate_shape {shape}")
         return shape
     if gate.shape == (1, D) or gate.shape == (D,):
         return LLEP_GATE_CHANNEL
@@ -480,8 +496,7 @@ def llep_block_norm_backward(r, b, gate, w_post, w_pre, alpha: float, eps: float
     _check(lib().llep_block_norm_backward(
         T, D, code, _ptr(r), _ptr(b), _ptr(gate), shape, _ptr(w_post), _ptr(w_pre), alpha, eps,
         _ptr(d_r), _ptr(d_h), _ptr(dx), _ptr(db), _ptr(d_gate), _ptr(dw_post), _ptr(dw_pre),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
-        "llep_block_norm_backward")
+        *_workspace(workspace), _stream(stream)), "llep_block_norm_backward")
 
 
 def llep_clip_gradients_workspace_bytes() -> int:
@@ -523,8 +538,8 @@ def llep_gradient_norm(grads, norm, workspace, stream=None):
     import torch
     _dense("norm", norm, (1,), torch.float32)
     _check(lib().llep_gradient_norm(len(grads), _gradients(grads, grads), _ptr(norm),
-                                    _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                    _stream(stream)), "llep_gradient_norm")
+                                    *_workspace(workspace), _stream(stream)),
+           "llep_gradient_norm")
 
 
 def llep_clip_gradients(grads, max_norm: float, norm, workspace, out=None, stream=None):
@@ -533,8 +548,7 @@ def llep_clip_gradients(grads, max_norm: float, norm, workspace, out=None, strea
     import torch
     _dense("norm", norm, (1,), torch.float32)
     _check(lib().llep_clip_gradients(len(grads), _gradients(grads, grads if out is None else out),
-                                     max_norm, _ptr(norm), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(),
+                                     max_norm, _ptr(norm), *_workspace(workspace),
                                      _stream(stream)), "llep_clip_gradients")
 
 
@@ -592,9 +606,8 @@ def llep_int8_matmul(x, x_scale, w_packed, w_scale, out, K: int, workspace=None,
     _dense("w_packed", w_packed, (1, lib().llep_packed_int8_bytes(1, N, K)), torch.int8)
     _dense("w_scale", w_scale, (N,), torch.float32)
     _dense("out", out, (M, N), out.dtype)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().llep_int8_matmul(M, N, K, _ptr(x), x.shape[-1], _ptr(x_scale), _ptr(w_packed),
-                                  _ptr(w_scale), code, _ptr(out), _ptr(workspace), nbytes,
+                                  _ptr(w_scale), code, _ptr(out), *_workspace(workspace),
                                   _stream(stream)), "llep_int8_matmul")
 
 
@@ -633,8 +646,7 @@ def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: i
     _check(getattr(lib(), name)(
         ctypes.byref(params), ctypes.byref(bufs.struct), device, _ptr(x_perm), _ptr(x_scale),
         _ptr(row_pair), _ptr(w_gate_up), _ptr(gate_scale), _ptr(up_scale), _ptr(w_down),
-        _ptr(down_scale), D, F, _ptr(out_perm), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)), name)
+        _ptr(down_scale), D, F, _ptr(out_perm), *_workspace(workspace), _stream(stream)), name)
 
 
 def llep_combine_to_bf16(params: llep_plan_params, out_perm, pair_row, topk_gates, y, stream=None):

@@ -98,6 +98,7 @@ class LLEPLayer:
         B.llep_plan(self.params, ids, self.bufs, stream)
 
     def permute(self, ids, gates, x, stream=None):
+        self.rows_are_int8 = False
         B.llep_permute(self.params, self.bufs, ids, gates, x, self.x_perm, self.gate_perm,
                        self.row_pair, self.pair_row, stream)
 
@@ -155,6 +156,9 @@ class LLEPLayer:
         if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
             raise ValueError("the experts do not fit this layer")
         self.gate_up_device = None
+        self.rows_are_int8 = True  # x_perm holds no rows of this call
+        if x_scale is None and tuple(x.shape) != (self.T, self.D):
+            raise ValueError("x does not fit this layer")
         if x_scale is None:
             B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
             x, x_scale = self.x_q, self.x_scale
@@ -198,6 +202,8 @@ class LLEPLayer:
         -1 the totals after the gradient return (experts without rows: zero).
         """
         import torch
+        if getattr(self, "rows_are_int8", False):
+            raise RuntimeError("backward() after forward_int8()")
         if not hasattr(self, "d_out_perm"):
             R = max(self.T * self.K, 1)
             dev, E, D, F = self.device, self.E, self.D, self.F

@@ -251,3 +251,44 @@ def test_serving_in_a_graph(dev):
             want_r = step(x.clone()).clone()
             torch.cuda.synchronize()
             assert torch.equal(got[0], want_r) and torch.equal(got[1], out)
+
+
+def test_misuse_is_refused(dev):
+    """What would read past a tensor, or another call's rows, raises."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    from paper_2601_17111_amd.layer import Int8Experts
+    T, D = 5, 64
+    x = torch.zeros((T, D), device=dev)
+    w = torch.ones(D, device=dev)
+    for gate, shape in [(torch.ones((1, D), device=dev), B.LLEP_GATE_FULL),
+                        (torch.ones((1, D), device=dev), B.LLEP_GATE_TOKEN),
+                        (torch.ones((T, 1), device=dev), B.LLEP_GATE_CHANNEL),
+                        (torch.ones((T, D), device=dev), B.LLEP_GATE_NONE),
+                        (torch.ones((T, D), device=dev), 9), (None, B.LLEP_GATE_FULL)]:
+        with pytest.raises(ValueError):
+            B.llep_block_norm(x, x.clone(), gate, w, w, 1.0, EPS, x.clone(), gate_shape=shape)
+    g = torch.ones(8, device=dev)
+    norm = torch.zeros(1, device=dev)
+    n = B.llep_clip_gradients_workspace_bytes()
+    for ws in (torch.zeros(n, dtype=torch.uint8), torch.zeros((n, 2), dtype=torch.uint8,
+                                                              device=dev)[:, 0]):
+        with pytest.raises(ValueError):
+            B.llep_gradient_norm([g], norm, ws)
+    with pytest.raises(B.LLEPError) as ei:
+        B.llep_gradient_norm([g], norm, None)
+    assert ei.value.code == B.LLEP_E_WORKSPACE
+    c = Case(dev, 8, "bf16", "none")
+    experts = Int8Experts.from_weights(*c.w)
+    c.block.forward_int8(c.ids, c.gates, c.x, experts)
+    with pytest.raises(RuntimeError):
+        c.block.backward(c.x, c.d_r, c.d_h, c.gates, c.packed[0], *c.packed_t)
+    with pytest.raises(ValueError):
+        c.block.layer.forward_int8(c.ids, c.gates, c.x[:, :32].contiguous(), experts)
+    with pytest.raises(ValueError):  # 8-bit rows of another width
+        c.block.layer.forward_int8(c.ids, c.gates, torch.zeros((8, 128), dtype=torch.int8,
+                                                               device=dev), experts, -1, None,
+                                   torch.zeros(8, device=dev))
+    c.block.forward(c.ids, c.gates, c.x, *c.packed)
+    c.block.backward(c.x, c.d_r, c.d_h, c.gates, c.packed[0], *c.packed_t)
+    torch.cuda.synchronize()
