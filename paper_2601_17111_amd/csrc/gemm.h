@@ -115,25 +115,27 @@ __device__ __forceinline__ float int8_swiglu(float g, float u) {
 __device__ __forceinline__ float int8_row_scale(const Int8GemmArgs &g, int64_t row) {
   return g.a_scale[g.row_pair ? int64_t(g.row_pair[row] / g.K) : row];
 }
-// four consecutive scales from column c on; columns from N on: 0
+// four consecutive scales from column c (a multiple of 4) on; columns from N
+// on: 0
 __device__ __forceinline__ f32x4 int8_col_scales(const float *s, int c, int N) {
-  if ((N & 3) == 0) {
-    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    return c < N ? *reinterpret_cast<const f32x4 *>(s + c) : zero;
-  }
+  if (c + 4 <= N) return *reinterpret_cast<const f32x4 *>(s + c);
   f32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = c + i < N ? s[c + i] : 0.0f;
   return v;
 }
 // four consecutive values of a row of C from column c on, those below N
+// (float32 rows of any length: 16-byte stores need 4-byte alignment alone)
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 template <typename Out>
 __device__ __forceinline__ void int8_store4(Out *row, int c, int N, const f32x4 v) {
-  if ((N & 3) == 0) {
-    if (c >= N) return;
-    if constexpr (sizeof(Out) == 4)
-      *reinterpret_cast<f32x4 *>(row + c) = v;
-    else
+  if constexpr (sizeof(Out) == 4) {
+    if (c + 4 <= N) {
+      *reinterpret_cast<f32x4_u *>(row + c) = v;
+      return;
+    }
+  } else if ((N & 3) == 0) {
+    if (c < N)
       *reinterpret_cast<uint2 *>(row + c) =
           make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     return;
