@@ -125,19 +125,18 @@ __device__ __forceinline__ f32x4 int8_col_scales(const float *s, int c, int N) {
   return v;
 }
 // four consecutive values of a row of C from column c on, those below N
-// (float32 rows of any length: 16-byte stores need 4-byte alignment alone)
+// (rows of any length: the compiler knows that the vectors are aligned to their
+// elements alone)
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(2)));
 template <typename Out>
 __device__ __forceinline__ void int8_store4(Out *row, int c, int N, const f32x4 v) {
-  if constexpr (sizeof(Out) == 4) {
-    if (c + 4 <= N) {
+  if (c + 4 <= N) {
+    if constexpr (sizeof(Out) == 4)
       *reinterpret_cast<f32x4_u *>(row + c) = v;
-      return;
-    }
-  } else if ((N & 3) == 0) {
-    if (c < N)
-      *reinterpret_cast<uint2 *>(row + c) =
-          make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    else
+      *reinterpret_cast<u32x2_u *>(row + c) =
+          u32x2_u{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     return;
   }
 #pragma unroll
