@@ -689,7 +689,9 @@ hipError_t launch_ffn_int8(const FfnInt8Args &a, hipStream_t stream) {
   q.x = act;
   q.q = act_q;
   q.scale = act_scale;
-  q.groups = a.groups;
+  // all devices: every row, without a look at the groups (a row that a bad id
+  // leaves empty is not read afterwards)
+  q.groups = a.device < 0 ? nullptr : a.groups;
   q.group_begin = a.group_begin;
   q.device = a.device;
   q.P = a.P;
