@@ -23,9 +23,26 @@ namespace llep {
 
 constexpr int kVec = 8;  // elements of a thread's vectors
 
+// kOdd: rows that are not whole 16-byte vectors, or not on 16-byte boundaries
+// (8192 x 2879 bf16 86 us; element by element 127).
+template <bool kOdd, typename T>
+__device__ __forceinline__ void fetch(RawVec<T, kVec> &v, const T *p, uint32_t left) {
+  if constexpr (kOdd)
+    v.load_any(p, int(left));
+  else
+    v.load(p);
+}
+template <bool kOdd, typename T>
+__device__ __forceinline__ void put(T *p, const float (&v)[kVec], uint32_t left) {
+  if constexpr (kOdd)
+    store_any<T, kVec>(p, v, int(left));
+  else
+    store_vec<T, kVec>(p, v);
+}
+
 // The weights of a thread's columns (norm weights, and the gate where it
 // varies by channel alone), read once per workgroup.
-template <typename T, int kPer>
+template <typename T, int kPer, bool kOdd>
 struct ColumnWeights {
   RawVec<T, kVec> post[kPer], pre[kPer], gate[kPer];
   __device__ __forceinline__ ColumnWeights(const NormArgs &a, uint32_t t, uint32_t n) {
@@ -36,15 +53,17 @@ struct ColumnWeights {
       pre[j].zero();
       gate[j].zero();
       if (c >= uint32_t(a.D)) continue;
-      if (a.w_post) post[j].load(static_cast<const T *>(a.w_post) + c);
-      if (a.w_pre) pre[j].load(static_cast<const T *>(a.w_pre) + c);
-      if (a.gate_shape == LLEP_GATE_CHANNEL) gate[j].load(static_cast<const T *>(a.gate) + c);
+      const uint32_t left = a.D - c;
+      if (a.w_post) fetch<kOdd>(post[j], static_cast<const T *>(a.w_post) + c, left);
+      if (a.w_pre) fetch<kOdd>(pre[j], static_cast<const T *>(a.w_pre) + c, left);
+      if (a.gate_shape == LLEP_GATE_CHANNEL)
+        fetch<kOdd>(gate[j], static_cast<const T *>(a.gate) + c, left);
     }
   }
 };
 
 // The gate's values of one row (requested with the row).
-template <typename T, int kPer>
+template <typename T, int kPer, bool kOdd>
 struct RowGate {
   RawVec<T, kVec> full[kPer];
   float token;
@@ -60,10 +79,11 @@ struct RowGate {
     for (int j = 0; j < kPer; ++j) {
       const uint32_t c = (j * n + t) * kVec;
       full[j].zero();
-      if (a.gate_shape == LLEP_GATE_FULL && c < uint32_t(a.D)) full[j].load(p + row * a.D + c);
+      if (a.gate_shape == LLEP_GATE_FULL && c < uint32_t(a.D))
+        fetch<kOdd>(full[j], p + row * a.D + c, a.D - c);
     }
   }
-  __device__ __forceinline__ float at(const NormArgs &a, const ColumnWeights<T, kPer> &w, int j,
+  __device__ __forceinline__ float at(const NormArgs &a, const ColumnWeights<T, kPer, kOdd> &w, int j,
                                       int i) const {
     return a.gate_shape == LLEP_GATE_CHANNEL ? w.gate[j][i]
            : a.gate_shape == LLEP_GATE_FULL  ? full[j][i]
@@ -71,7 +91,7 @@ struct RowGate {
   }
 };
 
-template <typename T, int kPer, bool kOne>
+template <typename T, int kPer, bool kOne, bool kOdd>
 __global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_kernel(NormArgs a) {
   __shared__ double lds[RowReduce<kOne>::kLds];
   RowReduce<kOne> red(lds);
@@ -85,7 +105,7 @@ __global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_ke
                            __builtin_amdgcn_readfirstlane(threadIdx.x / kWave)
                      : blockIdx.x;
   Raw x[kPer], b[kPer];
-  RowGate<T, kPer> gate;
+  RowGate<T, kPer, kOdd> gate;
   auto request = [&]() {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -93,13 +113,13 @@ __global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_ke
       x[j].zero();
       b[j].zero();
       if (c >= D) continue;
-      x[j].load(static_cast<const T *>(a.x) + row * D + c);
-      if (a.b) b[j].load(static_cast<const T *>(a.b) + row * D + c);
+      fetch<kOdd>(x[j], static_cast<const T *>(a.x) + row * D + c, D - c);
+      if (a.b) fetch<kOdd>(b[j], static_cast<const T *>(a.b) + row * D + c, D - c);
     }
     gate.load(a, row, t, n);
   };
   if (row < a.T) request();
-  const ColumnWeights<T, kPer> w(a, t, n);
+  const ColumnWeights<T, kPer, kOdd> w(a, t, n);
   while (row < a.T) {
     float r[kPer][kVec];
     if (a.b) {
@@ -133,7 +153,7 @@ __global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_ke
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
         const uint32_t c = (j * n + t) * kVec;
-        if (c < D) store_vec<T, kVec>(static_cast<T *>(a.r) + base + c, r[j]);
+        if (c < D) put<kOdd>(static_cast<T *>(a.r) + base + c, r[j], D - c);
       }
     }
     if (w_pre) {
@@ -149,7 +169,7 @@ __global__ __launch_bounds__(kOne ? kRowWaves * kWave : 1024) void block_norm_ke
         const uint32_t c = (j * n + t) * kVec;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) r[j][i] *= s * w.pre[j][i];
-        if (a.h && c < D) store_vec<T, kVec>(static_cast<T *>(a.h) + base + c, r[j]);
+        if (a.h && c < D) put<kOdd>(static_cast<T *>(a.h) + base + c, r[j], D - c);
       }
       if (a.h_q) {
         uint32_t most = 0;
@@ -189,7 +209,7 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
 #pragma unroll
     for (int i = 0; i < kVec; ++i) sum_pre[j][i] = sum_post[j][i] = 0.0f;
   Raw next_r[kPer], next_b[kPer], next_dr[kPer], next_dh[kPer];
-  RowGate<T, kPer> next_gate;
+  RowGate<T, kPer, false> next_gate;
   auto request = [&](int64_t row) {
     const int64_t base = row * D;
 #pragma unroll
@@ -211,13 +231,13 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
   };
   constexpr bool kAhead = kPer == 1;  // else there are no registers for it
   if (kAhead && blockIdx.x < a.n.T) request(blockIdx.x);
-  const ColumnWeights<T, kPer> w(a.n, t, n);
+  const ColumnWeights<T, kPer, false> w(a.n, t, n);
   for (int64_t row = blockIdx.x; row < a.n.T; row += gridDim.x) {
     if (!kAhead) request(row);
     const int64_t base = row * D;
     Raw r[kPer], b[kPer], dh[kPer];
     float dr[kPer][kVec];
-    const RowGate<T, kPer> gate = next_gate;
+    const RowGate<T, kPer, false> gate = next_gate;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       r[j] = next_r[j];
@@ -304,15 +324,13 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
   }
 }
 
-// ---------------------------------------------------------------------------
-// Odd rows: not whole 16-byte vectors, or not on 16-byte boundaries. Element by
-// element, several times over the row, which the cache holds; what has to stay
-// in 32 bits between two sweeps is kept in LDS, every element by its thread. In
+// Backward of odd rows: element by element, several times over the row, which
+// the cache holds; what has to stay in 32 bits between two sweeps is kept in
+// LDS, every element by its thread, and the column sums in the workspace. In
 // short rows a norm's gradient is the small rest of large terms (with one
-// element, f eps / (b^2 + eps)), so the backward, which need not be fast here,
-// has its row sums and what they enter in 64 bits.
-// ---------------------------------------------------------------------------
-
+// element, f eps / (b^2 + eps)), so the row sums and what they enter have 64
+// bits. (In registers, with 16-byte loads, the 64 bits take as long: 8192 x 2879
+// 260 and 264 us, 300 x 501 15 and 11.5.)
 template <typename T>
 __device__ __forceinline__ float load1(const void *p, int64_t i) {
   float v[1];
@@ -331,53 +349,6 @@ __device__ __forceinline__ float gate1(const NormArgs &a, int64_t row, int c) {
     case LLEP_GATE_TOKEN: return load1<T>(a.gate, row);
     case LLEP_GATE_FULL: return load1<T>(a.gate, row * a.D + c);
     default: return 1.0f;
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(1024) void block_norm_odd_kernel(NormArgs a) {
-  __shared__ double lds[RowReduce<false>::kLds];
-  __shared__ float kept[LLEP_MAX_NORM_DIM];
-  RowReduce<false> red(lds);
-  const int n = blockDim.x, t = threadIdx.x, D = a.D;
-  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
-    const int64_t base = row * D;
-    float s = a.alpha;
-    if (a.w_post) {
-      float q[1] = {0.0f};
-      for (int c = t; c < D; c += n) {
-        const float b = load1<T>(a.b, base + c);
-        q[0] = fmaf(b, b, q[0]);
-      }
-      red.sum(q);
-      s *= rsqrtf(q[0] / float(D) + a.eps);
-    }
-    float q[1] = {0.0f};
-    for (int c = t; c < D; c += n) {
-      float r = load1<T>(a.x, base + c);
-      if (a.b) {
-        const float g = gate1<T>(a, row, c);
-        r = fmaf(load1<T>(a.b, base + c) * s, a.w_post ? g * load1<T>(a.w_post, c) : g, r);
-      }
-      q[0] = fmaf(r, r, q[0]);
-      kept[c] = r;
-      if (a.r) store1<T>(a.r, base + c, r);
-    }
-    if (!a.w_pre) continue;
-    red.sum(q);
-    s = rsqrtf(q[0] / float(D) + a.eps);
-    uint32_t most = 0;
-    for (int c = t; c < D; c += n) {
-      const float h = kept[c] * (s * load1<T>(a.w_pre, c));
-      most = max(most, __float_as_uint(fabsf(h)));
-      kept[c] = h;
-      if (a.h) store1<T>(a.h, base + c, h);
-    }
-    if (!a.h_q) continue;
-    const RowScale s8 = row_scale(red.max_bits(most));
-    for (int c = t; c < a.q_bytes; c += n)
-      a.h_q[row * a.q_bytes + c] = c < D ? quantize(kept[c], s8) : int8_t(0);
-    if (t == 0) a.h_scale[row] = s8.scale;
   }
 }
 
@@ -486,9 +457,6 @@ bool rows_aligned(int32_t D, std::initializer_list<const void *> ps) {
 // 16384 x 2880 bf16 106 / 79 / 84 / 79 us, backward 131 / 119 / 146 / 147.)
 constexpr int kNormWaves = 16;
 
-// threads for a row of D elements, one by one
-static int odd_threads(int32_t D) { return std::min(1024, (D + kWave - 1) / kWave * kWave); }
-
 // at most `most` workgroups for n rows, with as many rows each
 static int64_t even_grid(int64_t n, int64_t most) {
   if (n <= most) return n;
@@ -496,12 +464,12 @@ static int64_t even_grid(int64_t n, int64_t most) {
   return (n + rows - 1) / rows;
 }
 
-template <typename T, int kPer, bool kOne>
+template <typename T, bool kOne, bool kOdd>
 hipError_t run_norm(const NormArgs &a, hipStream_t stream) {
-  const int threads = kOne ? kRowWaves * kWave : row_threads(a.D, kVec, kPer);
+  const int threads = kOne ? kRowWaves * kWave : row_threads(a.D, kVec, 1);
   const int64_t wgs = kOne ? (a.T + kRowWaves - 1) / kRowWaves : a.T;
   const int64_t grid = even_grid(wgs, int64_t(256) * std::max(1, kNormWaves * kWave / threads));
-  hipLaunchKernelGGL((block_norm_kernel<T, kPer, kOne>), dim3(uint32_t(grid)), dim3(threads), 0,
+  hipLaunchKernelGGL((block_norm_kernel<T, 1, kOne, kOdd>), dim3(uint32_t(grid)), dim3(threads), 0,
                      stream, a);
   return hipGetLastError();
 }
@@ -509,12 +477,11 @@ hipError_t run_norm(const NormArgs &a, hipStream_t stream) {
 template <typename T>
 hipError_t launch_norm_t(const NormArgs &a, hipStream_t stream) {
   static_assert(LLEP_MAX_NORM_DIM == 1024 * kVec, "a row fits a workgroup");
+  const bool one = a.D <= kWave * kVec;
   if (rows_aligned(a.D, {a.x, a.b, a.gate_shape == LLEP_GATE_TOKEN ? nullptr : a.gate, a.w_post,
                          a.w_pre, a.r, a.h}))
-    return a.D <= kWave * kVec ? run_norm<T, 1, true>(a, stream) : run_norm<T, 1, false>(a, stream);
-  hipLaunchKernelGGL(block_norm_odd_kernel<T>, dim3(uint32_t(std::min<int64_t>(a.T, 65536))),
-                     dim3(odd_threads(a.D)), 0, stream, a);
-  return hipGetLastError();
+    return one ? run_norm<T, true, false>(a, stream) : run_norm<T, false, false>(a, stream);
+  return one ? run_norm<T, true, true>(a, stream) : run_norm<T, false, true>(a, stream);
 }
 
 hipError_t launch_block_norm(const NormArgs &a, hipStream_t stream) {
@@ -548,7 +515,7 @@ hipError_t launch_norm_bwd_t(const NormBwdArgs &a, hipStream_t stream) {
     // 128 registers a thread, as 16 wavefronts have, hold a bf16 row's vectors
     // and the next row's; long float32 rows take half the threads
     if (!whole)
-      hipLaunchKernelGGL(block_norm_bwd_odd_kernel<T>, dim3(grid), dim3(odd_threads(D)), 0, stream,
+      hipLaunchKernelGGL(block_norm_bwd_odd_kernel<T>, dim3(grid), dim3(std::min(1024, (D + kWave - 1) / kWave * kWave)), 0, stream,
                          a);
     else if (D <= 512 * kVec)
       hipLaunchKernelGGL((block_norm_bwd_kernel<T, 1, 512>), dim3(grid),

@@ -45,6 +45,10 @@ __device__ __forceinline__ void load_vec(const T *p, float (&v)[kVec]) {
   }
 }
 
+// 16 bytes that are aligned to their elements alone.
+typedef int32_t i32x4_by2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef int32_t i32x4_by4 __attribute__((ext_vector_type(4), aligned(4)));
+
 // The same vector as it lies in memory, for rows that are read ahead of their
 // use, and as floats.
 template <typename T, int kVec>
@@ -60,6 +64,26 @@ struct RawVec {
   __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const Word *>(p)[i];
+  }
+  // of a row that starts anywhere (the compiler knows the vectors aligned to
+  // their elements alone): the first `left` elements, the others 0
+  __device__ __forceinline__ void load_any(const T *p, int left) {
+    static_assert(kVec == 8, "whole vectors, or a row's end");
+    using any = std::conditional_t<sizeof(T) == 2, i32x4_by2, i32x4_by4>;
+    if (left >= kVec) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const any *>(p)[i];
+      return;
+    }
+    zero();
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 2)
+          w[0][i / 2] |= int32_t(uint32_t(p[i]) << (16 * (i & 1)));
+        else
+          w[i / 4][i % 4] = __float_as_int(p[i]);
+      }
   }
   __device__ __forceinline__ float operator[](int i) const {  // i: known when compiled
     if constexpr (kVec == 1) {
@@ -95,6 +119,33 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[kVec]) {
       *reinterpret_cast<f32x4 *>(p + 4 * h) = q;
     }
   }
+}
+
+// The same for a row that starts anywhere: the first `left` elements.
+template <typename T, int kVec>
+__device__ __forceinline__ void store_any(T *p, const float (&v)[kVec], int left) {
+  using any = std::conditional_t<sizeof(T) == 2, i32x4_by2, i32x4_by4>;
+  if (left >= kVec) {
+    if constexpr (sizeof(T) == 2) {
+      i32x4 q;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = int32_t(pack_bf16x2(v[2 * i], v[2 * i + 1]));
+      *reinterpret_cast<any *>(p) = q;
+    } else {
+#pragma unroll
+      for (int h = 0; h < kVec / 4; ++h)
+        reinterpret_cast<any *>(p)[h] =
+            i32x4{__float_as_int(v[4 * h]), __float_as_int(v[4 * h + 1]),
+                  __float_as_int(v[4 * h + 2]), __float_as_int(v[4 * h + 3])};
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (i < left) {
+      const float x[1] = {v[i]};
+      store_vec<T, 1>(p + i, x);
+    }
 }
 
 // v of the lane that the DPP control names, or 0 where there is none
@@ -234,11 +285,11 @@ __device__ __forceinline__ void store_int8_row(int8_t *row, int32_t D, int32_t b
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int c = (j * n + t) * kVec;
-    if (c < D)
+    if (c < D)  // (8-bit rows are whole vectors; values from D on are 0)
       *reinterpret_cast<uint2 *>(row + c) =
           make_uint2(zero ? 0u : quantize4(v[j], s.inv), zero ? 0u : quantize4(v[j] + 4, s.inv));
   }
-  for (int c = D + t; c < bytes; c += n) row[c] = 0;
+  for (int c = (D + 7) / 8 * 8 + t; c < bytes; c += n) row[c] = 0;
 }
 
 }  // namespace llep
