@@ -254,13 +254,9 @@ __device__ __forceinline__ RowScale row_scale(float most) {
   return {most * (1.0f / 127.0f), 127.0f * (1.0f / most)};
 }
 
-__device__ __forceinline__ int8_t quantize(float v, RowScale s) {
-  return int8_t(s.inv != 0.0f ? rintf(v * s.inv) : 0.0f);  // at most 127: inv is rounded once
-}
-
 // Four at a time. v inv + 1.5 * 2^23 has rint(v inv) in its low byte (the sum
-// is rounded to a whole number, ties to even; the product before it, as above,
-// so the two are not contracted).
+// is rounded to a whole number, ties to even; the product is rounded before it,
+// so the two are not contracted). At most 127: inv is rounded once.
 __device__ __forceinline__ uint32_t quantize4(const float *v, float inv) {
 #pragma clang fp contract(off)
   uint32_t q[4];
