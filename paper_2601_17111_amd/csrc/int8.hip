@@ -486,7 +486,11 @@ void int8_tiles_kernel(Int8GemmArgs g) {
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
 hipError_t run_int8_tiles(const Int8GemmArgs &g, hipStream_t stream) {
-  const int grid = (cu_count() * (BM == 256 ? 1 : 2) + 7) / 8 * 8;
+  int64_t most = cu_count() * (BM == 256 ? 1 : 2);
+  // few dense tiles: as many workgroups, so that all XCDs have as many of them
+  // (2048^3 in 256 tiles 24 -> 15 us)
+  if (!kGrouped) most = std::min(most, (g.M + BM - 1) / BM * ((g.N + BN - 1) / BN));
+  const int grid = int((most + 7) / 8 * 8);
   hipLaunchKernelGGL((int8_tiles_kernel<BM, BN, WAVES_M, WAVES_N, kEpi, kGrouped>), dim3(grid),
                      dim3(64 * WAVES_M * WAVES_N), 0, stream, g);
   return hipGetLastError();
@@ -560,18 +564,27 @@ hipError_t launch_int8_matmul(const Int8MatmulArgs &a, hipStream_t stream) {
   g.b_scale = a.w_scale;
   g.M = a.M;
   g.f32_out = a.dtype == LLEP_F32;
-  // The ring's 256 x 256 tiles take about 1 us per 64 bytes of k however few
-  // there are, one on each compute unit, the stream 2.7 fs per multiply-add:
-  // 2048^3 40 / 22 us, 512 x 7168 x 2048 35 / 18, 512 x 2048 x 7168 66 / 18
-  // (tiles / stream).
-  const double tiles = double((a.M + 255) / 256) * double((a.N + 255) / 256);
-  const double ring = std::ceil(tiles / cu_count()) * (Kp / 64) * 1.0;
-  const double streamed = 2.7e-9 * double(a.M) * double(a.N) * double(a.K);
-  if (a.M <= 64 || streamed < ring) {
+  // The least of what the three ways take in us, about: the stream by its
+  // multiply-adds (rows in 64s) and outputs, the tiles by 64-byte slices of k and
+  // rounds of as many workgroups as the chip has room for (128 x 128 tiles: two
+  // on a compute unit, which take twice as long as one). Stream / 128 / 256 rows:
+  //   2048^3 21 / 15 / 25, 512 x 2048 x 7168 18 / 31 / 60, 512 x 7168 x 2048
+  //   17 / 14 / 24, 1024 x 7168 x 2048 30 / 22 / 26, 2048 x 2880 x 2880 35 / 26 / 32,
+  //   2000 x 4096 x 768 20 / 13 / 16, 6000 x 768 x 2048 28 / 20 / 25,
+  //   2048 x 7168 x 2048 57 / 42 / 33, 4096 x 2880 x 2880 66 / 55 / 38,
+  //   8192 x 7168 x 2048 220 / 146 / 131, 200 x 7168 x 7168 25 / 32 / 60
+  const double slices = Kp / 64, cus = cu_count(), m64 = double((a.M + 63) / 64 * 64);
+  auto tiles = [&](int64_t n) { return double((a.M + n - 1) / n) * double((a.N + n - 1) / n); };
+  const double streamed = 3 + m64 * double(a.N) * (1.0e-6 + 1.8e-9 * double(Kp));
+  const double ring128 = tiles(128) <= cus ? 5.5 + 0.25 * slices
+                                           : (4.5 + 0.5 * slices) * std::ceil(tiles(128) / (2 * cus));
+  const double ring256 = (12 + 0.65 * slices) * std::ceil(tiles(256) / cus);
+  if (a.M <= 64 || streamed < std::min(ring128, ring256)) {
     const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
     return launch_int8_stream<false, false>(g, rows, (a.M + rows - 1) / rows,
                                             int64_t(a.N) * Kp, stream);
   }
+  if (ring128 < ring256) return run_int8_tiles<128, 128, 2, 2, kEpiInt8, false>(g, stream);
   return run_int8_tiles<256, 256, kWavesM, kWavesN, kEpiInt8, false>(g, stream);
 }
 

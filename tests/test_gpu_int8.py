@@ -134,6 +134,20 @@ def test_product(dev, dtype, M, N, K):
     _check_product(dev, M, N, K, torch.bfloat16 if dtype == "bf16" else torch.float32, M + N + K)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [
+    # 128-row tiles: one to three slices of k and more, a last tile of few rows
+    # or columns, odd rows and columns, fewer tiles than workgroups and more
+    (1800, 1800, 64), (1793, 1801, 130), (130, 30001, 70), (1500, 3001, 501), (2050, 1288, 1300),
+    (2500, 4104, 200),
+    # 256-row tiles
+    (3000, 3001, 700), (3001, 5000, 1000),
+])
+def test_product_of_many_rows(dev, dtype, M, N, K):
+    import torch
+    _check_product(dev, M, N, K, torch.bfloat16 if dtype == "bf16" else torch.float32, M + N + K)
+
+
 @pytest.mark.parametrize("M", [1, 16, 20, 64, 65, 300])
 def test_largest_sums(dev, M):
     """Every product 127 * -127 over the largest k: whole numbers near 2^30."""
