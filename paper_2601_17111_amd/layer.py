@@ -22,11 +22,6 @@ def m_local_bytes(groups: Sequence[Sequence[int]], P: int, D: int, F: int,
     return out
 
 
-# Elements of the experts' outputs up to which forward_int8 keeps them in float32 (8 MB: a batch
-# of decoded tokens, where it costs nothing; prompts take 5-6% longer with it).
-INT8_WIDE_ELEMENTS = 1 << 21
-
-
 class Int8Experts:
     """Expert weights in 8 bits for LLEPLayer.forward_int8, packed once.
 
@@ -147,10 +142,10 @@ class LLEPLayer:
             self.x_q = torch.empty((self.T, self.D), **i8)
             self.x_scale = torch.empty(self.T, dtype=torch.float32, device=self.device)
             self.x_perm_q = torch.empty((max(self.T * self.K, 1), self.D), **i8)
-            # few outputs of the experts stay in float32, so that y is rounded once
-            R = max(self.T * self.K, 1)
-            self.out_perm_wide = None if R * self.D > INT8_WIDE_ELEMENTS else torch.empty(
-                (R, self.D), dtype=torch.float32, device=self.device)
+            # the experts' outputs stay in float32, so that y is rounded once in any batch (in
+            # bfloat16 a prompt takes 5% less, but its tokens lose bits and differ from decode's)
+            self.out_perm_wide = torch.empty((max(self.T * self.K, 1), self.D),
+                                             dtype=torch.float32, device=self.device)
             nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
             self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
@@ -167,13 +162,9 @@ class LLEPLayer:
         B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, x_scale,
                                 self.row_pair, experts.gate_up, experts.gate_scale,
                                 experts.up_scale, experts.down, experts.down_scale,
-                                self.out_perm if self.out_perm_wide is None else self.out_perm_wide,
-                                self.int8_workspace, stream)
-        if self.out_perm_wide is None:
-            self.combine(gates, stream)
-        else:
-            B.llep_combine_to_bf16(self.params, self.out_perm_wide, self.pair_row, gates, self.y,
-                                   stream)
+                                self.out_perm_wide, self.int8_workspace, stream)
+        B.llep_combine_to_bf16(self.params, self.out_perm_wide, self.pair_row, gates, self.y,
+                               stream)
         return self.y
 
     def _permute_int8(self, ids, gates, x, stream):
