@@ -407,6 +407,25 @@ def _all_dense(shape, dtype, tensors) -> bool:
     return True
 
 
+def _list(what: str, t, n: int, dtype):
+    """t, if it is a dense GPU tensor of this type with at least n elements along its only axis."""
+    if t is None:
+        raise ValueError(f"{what} is None")
+    _dense(what, t, t.shape, dtype)
+    if t.dim() != 1 or t.shape[0] < n:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not [{n}] or longer")
+    return t
+
+
+def _pairs(what: str, t, params: llep_plan_params, dtype):
+    """t, if it is a dense GPU tensor of this type with a value for every token-expert pair:
+    [T, K], or one after another."""
+    if t is None:
+        raise ValueError(f"{what} is None")
+    flat = t.dim() == 1
+    return _dense(what, t, (params.T * params.K,) if flat else (params.T, params.K), dtype)
+
+
 def _workspace(ws):
     """Pointer and bytes of a dense GPU tensor used as a workspace (or None)."""
     if ws is None:
@@ -628,13 +647,9 @@ def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: i
     if x_perm.shape[0] < R or out_perm.shape[0] < R:
         raise ValueError("x_perm and out_perm need T * K rows")
     _dense("x_perm", x_perm, (x_perm.shape[0], D), torch.int8)
-    _dense("x_scale", x_scale, (x_scale.shape[0],), torch.float32)
-    if x_scale.shape[0] < (R if row_pair is None else params.T):
-        raise ValueError("x_scale is too short")
+    _list("x_scale", x_scale, R if row_pair is None else params.T, torch.float32)
     if row_pair is not None:
-        _dense("row_pair", row_pair, (row_pair.shape[0],), torch.int32)
-        if row_pair.shape[0] < R:
-            raise ValueError("row_pair is too short")
+        _list("row_pair", row_pair, R, torch.int32)
     for what, t, n in (("gate_scale", gate_scale, F), ("up_scale", up_scale, F),
                        ("down_scale", down_scale, D)):
         _dense(what, t, (E, n), torch.float32)
@@ -650,11 +665,15 @@ def llep_grouped_ffn_int8(params: llep_plan_params, bufs: PlanBuffers, device: i
 
 
 def llep_combine_to_bf16(params: llep_plan_params, out_perm, pair_row, topk_gates, y, stream=None):
-    """llep_combine of float32 rows out_perm [T*K, D] into y [T, D] bf16."""
+    """llep_combine of float32 rows out_perm [T*K, D] into y [T, D] bf16: pair_row [T*K] int32,
+    topk_gates [T, K] float32 (or None: the pairs' sum)."""
     import torch
     D = out_perm.shape[-1]
     _dense("out_perm", out_perm, (out_perm.shape[0], D), torch.float32)
     _dense("y", y, (params.T, D), torch.bfloat16)
+    _list("pair_row", pair_row, params.T * params.K, torch.int32)
+    if topk_gates is not None:
+        _pairs("topk_gates", topk_gates, params, torch.float32)
     if out_perm.shape[0] < params.T * params.K:
         raise ValueError("out_perm needs T * K rows")
     _check(lib().llep_combine_to_bf16(ctypes.byref(params), _ptr(out_perm), _ptr(pair_row),

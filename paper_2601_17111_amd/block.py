@@ -33,6 +33,7 @@ class ExpertBlock:
 
     def forward(self, ids, gates, x, w_gate_up, w_down, stream=None):
         """Training forward (packed weights of llep_pack_weights). Returns (r, h_next)."""
+        self.layer.check_routing(ids, gates)
         B.llep_block_norm(x, None, None, None, self.w_pre, self.alpha, self.eps, None, self.h,
                           stream=stream)
         y = self.layer.forward(ids, gates, self.h, w_gate_up, w_down, -1, stream, True)
@@ -41,6 +42,7 @@ class ExpertBlock:
     def forward_int8(self, ids, gates, x, experts: Int8Experts, stream=None):
         """Serving forward with 8-bit experts (bf16 layers): the norm before them leaves its rows
         in 8 bits. Returns (r, h_next)."""
+        self.layer.check_routing(ids, gates)
         if not hasattr(self, "h_q"):
             import torch
             T, D = self.layer.T, self.layer.D
@@ -68,6 +70,7 @@ class ExpertBlock:
         (those that the block has)."""
         import torch
         T, D = self.layer.T, self.layer.D
+        B._pairs("gates", gates, self.layer.params, torch.float32)
         if not hasattr(self, "d_y"):
             dev = self.layer.device
             f32 = dict(dtype=torch.float32, device=dev)

@@ -127,6 +127,12 @@ class LLEPLayer:
         self.combine(gates, stream)
         return self.y
 
+    def check_routing(self, ids, gates):
+        """Refuses ids (int32) and gates (float32) that are not [T, K], or T K of them in order."""
+        import torch
+        B._pairs("ids", ids, self.params, torch.int32)
+        B._pairs("gates", gates, self.params, torch.float32)
+
     def forward_int8(self, ids, gates, x, experts: Int8Experts, device: int = -1, stream=None,
                      x_scale=None):
         """forward() for serving with 8-bit experts (bf16 layers): the tokens to 8 bits, then
@@ -150,6 +156,7 @@ class LLEPLayer:
             self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
             raise ValueError("the experts do not fit this layer")
+        self.check_routing(ids, gates)
         self.gate_up_device = None
         self.rows_are_int8 = True  # x_perm holds no rows of this call
         if x_scale is None and tuple(x.shape) != (self.T, self.D):
