@@ -260,14 +260,17 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
     if (has_pre || has_post) red.sum(q);
     const float i_b = has_post ? rsqrtf(q[2] * per_d + a.n.eps) : 1.0f;
     if (has_pre) {
+      // one factor at a time: i_r^3 leaves the range of 32 bits for rows of 1e13
+      // (and 1e-13) and more
       const float i_r = rsqrtf(q[0] * per_d + a.n.eps);
-      const float k = i_r * i_r * i_r * (q[1] * per_d);
+      const float k = i_r * (q[1] * per_d);
 #pragma unroll
       for (int j = 0; j < kPer; ++j)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-          sum_pre[j][i] = fmaf(dh[j][i], r[j][i] * i_r, sum_pre[j][i]);
-          dr[j][i] += fmaf(i_r, dh[j][i] * w.pre[j][i], -k * r[j][i]);
+          const float ri = r[j][i] * i_r;
+          sum_pre[j][i] = fmaf(dh[j][i], ri, sum_pre[j][i]);
+          dr[j][i] = fmaf(i_r, fmaf(dh[j][i], w.pre[j][i], -k * ri), dr[j][i]);
         }
     }
 #pragma unroll
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
     float k = 0.0f;
     if (has_post || a.n.gate_shape == LLEP_GATE_TOKEN) {
       red.sum(p);
-      if (has_post) k = i_b * i_b * (p[0] * per_d);
+      if (has_post) k = i_b * (p[0] * per_d);
       if (a.n.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = p[1];
     }
     const float s = a.n.alpha * i_b;
@@ -307,7 +310,7 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
     for (int j = 0; j < kPer; ++j) {
       const uint32_t c = (j * n + t) * kVec;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dr[j][i] = s * fmaf(-k, b[j][i], dr[j][i]);
+      for (int i = 0; i < kVec; ++i) dr[j][i] = s * fmaf(-k, b[j][i] * i_b, dr[j][i]);
       if (c < D) store_vec<T, kVec>(static_cast<T *>(a.db) + base + c, dr[j]);
     }
   }
