@@ -305,12 +305,14 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
       if (has_post) k = i_b * (p[0] * per_d);
       if (a.n.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = p[1];
     }
+    // (without w_post b does not enter db, whatever is in it)
     const float s = a.n.alpha * i_b;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const uint32_t c = (j * n + t) * kVec;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dr[j][i] = s * fmaf(-k, b[j][i] * i_b, dr[j][i]);
+      for (int i = 0; i < kVec; ++i)
+        dr[j][i] = s * (has_post ? fmaf(-k, b[j][i] * i_b, dr[j][i]) : dr[j][i]);
       if (c < D) store_vec<T, kVec>(static_cast<T *>(a.db) + base + c, dr[j]);
     }
   }
@@ -406,9 +408,11 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_odd_kernel(NormBwdArgs a)
     red.sum(p);
     if (f.gate_shape == LLEP_GATE_TOKEN && t == 0) a.d_gate[row] = float(p[1]);
     k = f.w_post ? i_b * i_b * (p[0] / D) : 0.0;
-    for (int c = t; c < D; c += n)
-      store1<T>(a.db, base + c, float(double(f.alpha) * i_b *
-                                      (double(kept[c]) - k * double(load1<T>(f.b, base + c)))));
+    for (int c = t; c < D; c += n) {
+      double d = kept[c];
+      if (f.w_post) d -= k * double(load1<T>(f.b, base + c));
+      store1<T>(a.db, base + c, float(double(f.alpha) * i_b * d));
+    }
   }
 }
 

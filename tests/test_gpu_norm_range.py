@@ -63,3 +63,29 @@ def test_large_and_small_rows(dev, dtype, D, off):
     assert (np.abs(_np(dpre) - want["dw_pre"]) <= 2e-5 * terms).all()
     terms = np.abs(0.5 * want["dx"] * oracle.rms_norm(_np(b), 0.0)).sum(0)
     assert (np.abs(_np(dpost) - want["dw_post"]) <= 2e-5 * terms).all()
+
+
+@pytest.mark.parametrize("D", [64, 33])
+@pytest.mark.parametrize("gate", ["none", "channel", "token", "full"])
+def test_outputs_not_finite_without_their_norm(dev, gate, D):
+    """Without w_post, db = alpha gate dx has nothing of b: an infinity or a NaN there (of a place
+    that the next step masks, say) reaches neither db nor dx."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    T = 3
+    g = torch.Generator().manual_seed(D)
+    b = torch.randn((T, D), generator=g).to(dev)
+    b[0, 3], b[1, 0], b[2, D - 1] = float("inf"), -float("inf"), float("nan")
+    shape = {"none": None, "channel": (1, D), "token": (T, 1), "full": (T, D)}[gate]
+    gt = None if shape is None else torch.randn(shape, generator=g).to(dev)
+    d_r = torch.randn((T, D), generator=g).to(dev)
+    dx, db = torch.empty_like(b), torch.empty_like(b)
+    d_gate = None if gt is None else torch.empty_like(gt)
+    ws = torch.empty(B.llep_block_norm_backward_workspace_bytes(T, D), dtype=torch.uint8,
+                     device=dev)
+    B.llep_block_norm_backward(None, b, gt, None, None, 0.5, 1e-5, d_r, None, dx, db, d_gate, None,
+                               None, ws, gate_shape=dict(none=0, channel=1, token=2, full=3)[gate])
+    torch.cuda.synchronize()
+    assert torch.equal(dx, d_r)
+    want = 0.5 * d_r * (1.0 if gt is None else gt)
+    assert bool(((db - want).abs() <= 2.0 ** -22 * want.abs()).all())
