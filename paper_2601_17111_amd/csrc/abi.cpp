@@ -677,8 +677,9 @@ static int grouped_ffn_int8(const llep_plan_params *params, const llep_plan_buff
   if ((rc = check_plan_buffers(plan)) != LLEP_OK) return rc;
   if ((rc = check_ffn_dims(D, F, LLEP_BF16)) != LLEP_OK) return rc;
   if (device < -1 || device >= params->P) return fail(LLEP_E_ARG, "device outside [-1, P)");
-  if (!x_perm || !x_scale || !w_gate_up_packed || !gate_scale || !up_scale || !w_down_packed ||
-      !down_scale || !out_perm)
+  // (arrays of no rows may have no address)
+  if (!w_gate_up_packed || !gate_scale || !up_scale || !w_down_packed || !down_scale ||
+      (params->T > 0 && (!x_perm || !x_scale || !out_perm)))
     return fail(LLEP_E_ARG, "a data pointer is null");
   if (!aligned16(x_perm) || !aligned16(w_gate_up_packed) || !aligned16(w_down_packed) ||
       !aligned16(gate_scale) || !aligned16(up_scale) || !aligned16(down_scale) ||
