@@ -70,6 +70,7 @@ class ExpertBlock:
         (those that the block has)."""
         import torch
         T, D = self.layer.T, self.layer.D
+        self.layer.check_backward()
         B._pairs("gates", gates, self.layer.params, torch.float32)
         if not hasattr(self, "d_y"):
             dev = self.layer.device

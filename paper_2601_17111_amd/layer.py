@@ -37,6 +37,12 @@ class Int8Experts:
         if (tuple(gate_scale.shape) != (E, F) or tuple(up_scale.shape) != (E, F)
                 or tuple(down_scale.shape) != (E, D)):
             raise ValueError("scales are [E, F], [E, F] and [E, D]")
+        import torch
+        for what, t in (("gate_scale", gate_scale), ("up_scale", up_scale),
+                        ("down_scale", down_scale)):
+            B._dense(what, t, t.shape, torch.float32)
+            if t.data_ptr() % 16:
+                raise ValueError(f"{what} does not start on a 16-byte boundary")
         self.E, self.D, self.F = E, D, F
         self.gate_up = B.llep_pack_matrix_int8(w_gate, w_up, stream)
         self.down = B.llep_pack_matrix_int8(w_down, stream=stream)
@@ -136,34 +142,34 @@ class LLEPLayer:
     def forward_int8(self, ids, gates, x, experts: Int8Experts, device: int = -1, stream=None,
                      x_scale=None):
         """forward() for serving with 8-bit experts (bf16 layers): the tokens to 8 bits, then
-        plan -> permute (of the 8-bit rows) -> grouped FFN in 8 bits -> combine. Returns y.
+        plan -> permute (of the 8-bit rows) -> grouped FFN in 8 bits -> combine. Returns y (valid
+        for every token only when device == -1).
         x [T, D] may already be 8-bit rows (int8), with their x_scale [T] (llep_block_norm and
-        llep_quantize_rows write both). backward() is not available after it."""
-        if not hasattr(self, "x_q"):
-            import torch
-            if self.dtype != torch.bfloat16:
-                raise TypeError("forward_int8 needs a bf16 layer")
-            i8 = dict(dtype=torch.int8, device=self.device)
-            B.llep_int8_row_bytes(self.D)  # refuses what the 8-bit calls would
-            self.x_q = torch.empty((self.T, self.D), **i8)
-            self.x_scale = torch.empty(self.T, dtype=torch.float32, device=self.device)
-            self.x_perm_q = torch.empty((max(self.T * self.K, 1), self.D), **i8)
-            # the experts' outputs stay in float32, so that y is rounded once in any batch (in
-            # bfloat16 a prompt takes 5% less, but its tokens lose bits and differ from decode's)
-            self.out_perm_wide = torch.empty((max(self.T * self.K, 1), self.D),
-                                             dtype=torch.float32, device=self.device)
-            nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
-            self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        llep_quantize_rows write both). backward() is not available after it; a call that is
+        refused changes nothing."""
+        import torch
+        if self.dtype != torch.bfloat16:
+            raise TypeError("forward_int8 needs a bf16 layer")
         if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
             raise ValueError("the experts do not fit this layer")
+        if not -1 <= device < self.P:
+            raise ValueError("device outside [-1, P)")
         self.check_routing(ids, gates)
-        self.gate_up_device = None
-        self.rows_are_int8 = True  # x_perm holds no rows of this call
-        if x_scale is None and tuple(x.shape) != (self.T, self.D):
-            raise ValueError("x does not fit this layer")
+        if x_scale is None:
+            B._dense("x", x, (self.T, self.D), x.dtype)
+            B._dtype_code(x)
+        else:
+            B._dense("x", x, (self.T, self.D), torch.int8)
+            B._list("x_scale", x_scale, self.T, torch.float32)
+            if x.data_ptr() % 16:
+                raise ValueError("x does not start on a 16-byte boundary")
+        if not hasattr(self, "int8_workspace"):
+            self._make_int8_buffers()
         if x_scale is None:
             B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
             x, x_scale = self.x_q, self.x_scale
+        self.gate_up_device = None
+        self.rows_are_int8 = True  # x_perm holds no rows of this call
         self.plan(ids, stream)
         self._permute_int8(ids, gates, x, stream)
         B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, x_scale,
@@ -174,10 +180,26 @@ class LLEPLayer:
                                stream)
         return self.y
 
+    def _make_int8_buffers(self):
+        import torch
+        R = max(self.T * self.K, 1)
+        i8 = dict(dtype=torch.int8, device=self.device)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        if self.D % 64 or self.F % 64 or max(self.D, self.F) > B.LLEP_MAX_FFN_DIM:
+            raise B.LLEPError(B.LLEP_E_ARG, "forward_int8",
+                              "D and F must be multiples of 64, at most LLEP_MAX_FFN_DIM")
+        self.x_q = torch.empty((self.T, self.D), **i8)
+        self.x_scale = torch.empty(self.T, **f32)
+        self.x_perm_q = torch.empty((R, self.D), **i8)
+        # the experts' outputs stay in float32, so that y is rounded once in any batch (in bfloat16
+        # a prompt takes 5% less, but its tokens lose bits and differ from decode's)
+        self.out_perm_wide = torch.empty((R, self.D), **f32)
+        nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
+        self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
     def _permute_int8(self, ids, gates, x, stream):
         """The permutation of rows of D bytes, as D / 2 bfloat16."""
         import torch
-        B._dense("x", x, (self.T, self.D), torch.int8)
         B.llep_permute(self.params, self.bufs, ids, gates, x.view(torch.bfloat16),
                        self.x_perm_q.view(torch.bfloat16), self.gate_perm, self.row_pair,
                        self.pair_row, stream)
@@ -185,6 +207,11 @@ class LLEPLayer:
     def _saved_covers(self, device: int) -> bool:
         saved = getattr(self, "gate_up_device", None)
         return saved is not None and (saved == -1 or saved == device)
+
+    def check_backward(self):
+        """Refuses a backward() whose rows forward_int8() has replaced."""
+        if getattr(self, "rows_are_int8", False):
+            raise RuntimeError("backward() after forward_int8()")
 
     def backward(self, dy, gates, w_gate_up, w_gate_up_t, w_down_t, device: int = -1,
                  stream=None):
@@ -200,8 +227,7 @@ class LLEPLayer:
         -1 the totals after the gradient return (experts without rows: zero).
         """
         import torch
-        if getattr(self, "rows_are_int8", False):
-            raise RuntimeError("backward() after forward_int8()")
+        self.check_backward()
         if not hasattr(self, "d_out_perm"):
             R = max(self.T * self.K, 1)
             dev, E, D, F = self.device, self.E, self.D, self.F
