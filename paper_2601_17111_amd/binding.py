@@ -183,6 +183,19 @@ def _stream(stream=None) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _empty(shape, dtype, device, stream=None):
+    """torch.empty for a call on `stream` (None: the current one). The memory is that stream's, as
+    the current stream's could still be in use by what is enqueued there, and is not given away,
+    once freed, before the current stream is done with it too."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _dtype_code(t) -> int:
     import torch
     if t.dtype == torch.bfloat16:
@@ -274,12 +287,11 @@ def llep_pack_weights(w_gate, w_up, w_down, stream=None, out=None):
     """Packed copies of the expert weights (see llep.h); returns (gate_up, down).
     `out` = (gate_up, down) packs into those (contiguous) tensors instead, e.g.
     slices of a larger packed set filled a few experts at a time."""
-    import torch
     E, D, F = w_gate.shape
     code = _dtype_code(w_gate)
     if out is None:
-        gu = torch.empty((E, 2 * F, D), dtype=w_gate.dtype, device=w_gate.device)
-        dn = torch.empty((E, D, F), dtype=w_gate.dtype, device=w_gate.device)
+        gu = _empty((E, 2 * F, D), w_gate.dtype, w_gate.device, stream)
+        dn = _empty((E, D, F), w_gate.dtype, w_gate.device, stream)
     else:
         gu, dn = out
         if (gu.numel() != E * 2 * F * D or dn.numel() != E * D * F or not gu.is_contiguous()
@@ -346,10 +358,9 @@ def llep_combine_backward(params: llep_plan_params, out_perm, pair_row, topk_gat
 def llep_pack_weights_backward(w_gate, w_up, w_down, stream=None):
     """Packed weights of the backward GEMMs (see llep.h); returns
     (gate_up_t, down_t)."""
-    import torch
     E, D, F = w_gate.shape
-    gut = torch.empty((E, D, 2 * F), dtype=w_gate.dtype, device=w_gate.device)
-    dnt = torch.empty((E, F, D), dtype=w_gate.dtype, device=w_gate.device)
+    gut = _empty((E, D, 2 * F), w_gate.dtype, w_gate.device, stream)
+    dnt = _empty((E, F, D), w_gate.dtype, w_gate.device, stream)
     _check(lib().llep_pack_weights_backward(E, D, F, _dtype_code(w_gate), _ptr(w_gate),
                                             _ptr(w_up), _ptr(w_down), _ptr(gut), _ptr(dnt),
                                             _stream(stream)), "llep_pack_weights_backward")
@@ -604,7 +615,7 @@ def llep_pack_matrix_int8(w, w_up=None, stream=None):
     _dense("w", w, w.shape, torch.int8)
     _dense("w_up", w_up, w.shape, torch.int8)
     nbytes = lib().llep_packed_int8_bytes(E, N, K) * (1 if w_up is None else 2)
-    out = torch.empty((E, nbytes // E), dtype=torch.int8, device=w.device)
+    out = _empty((E, nbytes // E), torch.int8, w.device, stream)
     _check(lib().llep_pack_int8(E, N, K, _ptr(w), _ptr(w_up), _ptr(out), _stream(stream)),
            "llep_pack_int8")
     return out

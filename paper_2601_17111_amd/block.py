@@ -17,7 +17,8 @@ class ExpertBlock:
 
     x, r, h, h_next [T, D] in the layer's type; w_pre, w_post, w_next [D] and
     gate ([1, D], [T, 1], [T, D] or None) in the same type. w_post or w_next may
-    be None (no norm after the experts; no norm before a next block).
+    be None (no norm after the experts; no norm before a next block). Buffers
+    and streams as in LLEPLayer.
     """
 
     def __init__(self, layer: LLEPLayer, w_pre, w_post=None, gate=None, w_next=None,
@@ -46,8 +47,8 @@ class ExpertBlock:
         if not hasattr(self, "h_q"):
             import torch
             T, D = self.layer.T, self.layer.D
-            self.h_q = torch.empty((T, D), dtype=torch.int8, device=self.layer.device)
-            self.h_scale = torch.empty(T, dtype=torch.float32, device=self.layer.device)
+            self.h_q = B._empty((T, D), torch.int8, self.layer.device, stream)
+            self.h_scale = B._empty((T,), torch.float32, self.layer.device, stream)
         B.llep_block_norm(x, None, None, None, self.w_pre, self.alpha, self.eps, None, None,
                           self.h_q, self.h_scale, stream)
         y = self.layer.forward_int8(ids, gates, self.h_q, experts, -1, stream, self.h_scale)
@@ -74,14 +75,13 @@ class ExpertBlock:
         B._pairs("gates", gates, self.layer.params, torch.float32)
         if not hasattr(self, "d_y"):
             dev = self.layer.device
-            f32 = dict(dtype=torch.float32, device=dev)
-            row = dict(dtype=self.layer.dtype, device=dev)
-            self.d_x, self.d_res, self.d_y = (torch.empty((T, D), **row) for _ in range(3))
-            self.d_w = {k: torch.empty(w.shape, **f32) for k, w in
+            self.d_x, self.d_res, self.d_y = (
+                B._empty((T, D), self.layer.dtype, dev, stream) for _ in range(3))
+            self.d_w = {k: B._empty(w.shape, torch.float32, dev, stream) for k, w in
                         (("w_pre", self.w_pre), ("w_post", self.w_post), ("gate", self.gate),
                          ("w_next", self.w_next)) if w is not None}
             nbytes = B.llep_block_norm_backward_workspace_bytes(T, D)
-            self.norm_workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+            self.norm_workspace = B._empty((max(nbytes, 16),), torch.uint8, dev, stream)
         g = self.d_w
         B.llep_block_norm_backward(self.r, self.layer.y, self.gate, self.w_post, self.w_next,
                                    self.alpha, self.eps, d_r, d_h_next, self.d_res, self.d_y,
@@ -99,9 +99,9 @@ class ExpertBlock:
         import torch
         if not hasattr(self, "grad_norm"):
             dev = self.layer.device
-            self.grad_norm = torch.empty(1, dtype=torch.float32, device=dev)
-            self.clip_workspace = torch.empty(B.llep_clip_gradients_workspace_bytes(),
-                                              dtype=torch.uint8, device=dev)
+            self.grad_norm = B._empty((1,), torch.float32, dev, stream)
+            self.clip_workspace = B._empty((B.llep_clip_gradients_workspace_bytes(),),
+                                           torch.uint8, dev, stream)
         B.llep_clip_gradients(list(grads.values()), max_norm, self.grad_norm, self.clip_workspace,
                               stream=stream)
         return self.grad_norm

@@ -70,6 +70,8 @@ class LLEPLayer:
 
     ids [T, K] int32, gates [T, K] float32, x [T, D] (bf16 or f32) are device
     tensors; w_gate_up / w_down are the packed weights (llep_pack_weights).
+    The buffers made here are the current stream's: another stream that calls
+    are given has to wait for it first. Those that a call makes are its stream's.
     """
 
     def __init__(self, T: int, K: int, E: int, P: int, D: int, F: int, capacity: int,
@@ -108,9 +110,8 @@ class LLEPLayer:
         not recompute them."""
         if save_gate_up:
             if getattr(self, "gate_up", None) is None:
-                import torch
-                self.gate_up = torch.empty((max(self.T * self.K, 1), 2 * self.F),
-                                           dtype=self.dtype, device=self.device)
+                self.gate_up = B._empty((max(self.T * self.K, 1), 2 * self.F), self.dtype,
+                                        self.device, stream)
             B.llep_grouped_ffn_train(self.params, self.bufs, device, self.x_perm, w_gate_up,
                                      w_down, self.out_perm, self.gate_up, self.workspace, stream)
             self.gate_up_device = device
@@ -164,7 +165,7 @@ class LLEPLayer:
             if x.data_ptr() % 16:
                 raise ValueError("x does not start on a 16-byte boundary")
         if not hasattr(self, "int8_workspace"):
-            self._make_int8_buffers()
+            self._make_int8_buffers(stream)
         if x_scale is None:
             B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
             x, x_scale = self.x_q, self.x_scale
@@ -180,22 +181,20 @@ class LLEPLayer:
                                stream)
         return self.y
 
-    def _make_int8_buffers(self):
+    def _make_int8_buffers(self, stream):
         import torch
-        R = max(self.T * self.K, 1)
-        i8 = dict(dtype=torch.int8, device=self.device)
-        f32 = dict(dtype=torch.float32, device=self.device)
-        if self.D % 64 or self.F % 64 or max(self.D, self.F) > B.LLEP_MAX_FFN_DIM:
+        R, D, dev = max(self.T * self.K, 1), self.D, self.device
+        if D % 64 or self.F % 64 or max(D, self.F) > B.LLEP_MAX_FFN_DIM:
             raise B.LLEPError(B.LLEP_E_ARG, "forward_int8",
                               "D and F must be multiples of 64, at most LLEP_MAX_FFN_DIM")
-        self.x_q = torch.empty((self.T, self.D), **i8)
-        self.x_scale = torch.empty(self.T, **f32)
-        self.x_perm_q = torch.empty((R, self.D), **i8)
+        self.x_q = B._empty((self.T, D), torch.int8, dev, stream)
+        self.x_scale = B._empty((self.T,), torch.float32, dev, stream)
+        self.x_perm_q = B._empty((R, D), torch.int8, dev, stream)
         # the experts' outputs stay in float32, so that y is rounded once in any batch (in bfloat16
         # a prompt takes 5% less, but its tokens lose bits and differ from decode's)
-        self.out_perm_wide = torch.empty((R, self.D), **f32)
+        self.out_perm_wide = B._empty((R, D), torch.float32, dev, stream)
         nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
-        self.int8_workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.int8_workspace = B._empty((nbytes,), torch.uint8, dev, stream)
 
     def _permute_int8(self, ids, gates, x, stream):
         """The permutation of rows of D bytes, as D / 2 bfloat16."""
@@ -231,16 +230,16 @@ class LLEPLayer:
         if not hasattr(self, "d_out_perm"):
             R = max(self.T * self.K, 1)
             dev, E, D, F = self.device, self.E, self.D, self.F
-            self.d_out_perm = torch.empty((R, D), dtype=self.dtype, device=dev)
-            self.dx_perm = torch.empty((R, D), dtype=self.dtype, device=dev)
-            self.d_gates = torch.empty((self.T, self.K), dtype=torch.float32, device=dev)
-            self.dx = torch.empty((self.T, D), dtype=self.dtype, device=dev)
-            self.dw_gate = torch.empty((E, D, F), dtype=torch.float32, device=dev)
-            self.dw_up = torch.empty((E, D, F), dtype=torch.float32, device=dev)
-            self.dw_down = torch.empty((E, F, D), dtype=torch.float32, device=dev)
+            self.d_out_perm = B._empty((R, D), self.dtype, dev, stream)
+            self.dx_perm = B._empty((R, D), self.dtype, dev, stream)
+            self.d_gates = B._empty((self.T, self.K), torch.float32, dev, stream)
+            self.dx = B._empty((self.T, D), self.dtype, dev, stream)
+            self.dw_gate = B._empty((E, D, F), torch.float32, dev, stream)
+            self.dw_up = B._empty((E, D, F), torch.float32, dev, stream)
+            self.dw_down = B._empty((E, F, D), torch.float32, dev, stream)
             code = B.LLEP_BF16 if self.dtype == torch.bfloat16 else B.LLEP_F32
             nbytes = B.llep_grouped_ffn_backward_workspace_bytes(self.params, D, F, code)
-            self.bwd_workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            self.bwd_workspace = B._empty((nbytes,), torch.uint8, dev, stream)
         B.llep_zero_absent_gradients(self.params, self.bufs, device, self.dw_gate, self.dw_up,
                                      self.dw_down, stream)
         B.llep_combine_backward(self.params, self.out_perm, self.pair_row, gates, dy,
