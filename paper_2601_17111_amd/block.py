@@ -15,7 +15,8 @@ class ExpertBlock:
     """h = norm(x) w_pre;  y = experts(h);  r = x + alpha gate norm(y) w_post;
     h_next = norm(r) w_next.
 
-    x, r, h, h_next [T, D] in the layer's type; w_pre, w_post, w_next [D] and
+    x, r, h, h_next [T, D] in the layer's type, D at most LLEP_MAX_NORM_DIM
+    (layers on their own take longer rows); w_pre, w_post, w_next [D] and
     gate ([1, D], [T, 1], [T, D] or None) in the same type. w_post or w_next may
     be None (no norm after the experts; no norm before a next block). Buffers
     and streams as in LLEPLayer.
@@ -27,6 +28,8 @@ class ExpertBlock:
         self.layer, self.alpha, self.eps = layer, alpha, eps
         self.w_pre, self.w_post, self.gate, self.w_next = w_pre, w_post, gate, w_next
         T, D = layer.T, layer.D
+        if D > B.LLEP_MAX_NORM_DIM:
+            raise ValueError(f"the norms take rows of up to {B.LLEP_MAX_NORM_DIM} elements, not {D}")
         row = dict(dtype=layer.dtype, device=layer.device)
         self.h = torch.empty((T, D), **row)
         self.r = torch.empty((T, D), **row)
