@@ -615,6 +615,8 @@ def llep_pack_matrix_int8(w, w_up=None, stream=None):
     _dense("w", w, w.shape, torch.int8)
     _dense("w_up", w_up, w.shape, torch.int8)
     nbytes = lib().llep_packed_int8_bytes(E, N, K) * (1 if w_up is None else 2)
+    if nbytes == 0:
+        raise LLEPError(LLEP_E_ARG, "llep_pack_matrix_int8", "E, N or K outside its range")
     out = _empty((E, nbytes // E), torch.int8, w.device, stream)
     _check(lib().llep_pack_int8(E, N, K, _ptr(w), _ptr(w_up), _ptr(out), _stream(stream)),
            "llep_pack_int8")
