@@ -548,7 +548,7 @@ def _gradients(grads, out):
     both = (grads,) if out is grads else (grads, out)
     if (None in codes or not all(all(map(T.is_contiguous, ts)) and all(map(_IS_CUDA, ts))
                                  for ts in both)
-            or (out is not grads and (list(map(T.numel, out)) != sizes
+            or (out is not grads and (not all(map(T.is_same_size, out, grads))
                                       or list(map(_DTYPE_OF, out)) != types))):
         for i, (g, o) in enumerate(zip(grads, out)):
             _dtype_code(g)
