@@ -538,11 +538,13 @@ typedef struct {
  * in 64 bits in a fixed order (no float32 gradient overflows it).
  * llep_clip_gradients also writes, with that norm,
  *   out = g * min(1, max_norm / norm)
- * (in 32 bits, rounded once to the tensor's dtype). A norm that is infinite or
- * NaN, or at most max_norm, leaves every gradient as it is: norm tells the
- * caller, who then skips the step. Outputs may be the inputs, but may not
- * overlap them otherwise, nor each other. No tensors: norm = 0. Workspace of
- * llep_clip_gradients_workspace_bytes() bytes, 16-byte aligned, for both.
+ * (in 32 bits, rounded once to the tensor's dtype). A norm that is infinite in
+ * float32 (of gradients that are, or of finite ones beyond its range) or NaN, or
+ * at most max_norm, leaves every gradient as it is, whatever max_norm / norm
+ * would be: norm tells the caller, who then skips the step. Outputs may be the
+ * inputs, but may not overlap them otherwise, nor each other. No tensors: norm =
+ * 0. Workspace of llep_clip_gradients_workspace_bytes() bytes, 16-byte aligned,
+ * for both.
  * Errors: LLEP_E_ARG, LLEP_E_DTYPE, LLEP_E_WORKSPACE. */
 size_t llep_clip_gradients_workspace_bytes(void);
 int llep_gradient_norm(int32_t n, const llep_gradient *grads, float *norm,

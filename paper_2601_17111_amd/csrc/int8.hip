@@ -11,7 +11,7 @@
 //     through a ring in LDS, bound by the matrix cores, which are 85% busy at the
 //     clock that the power limit leaves them (8192^3 490 us, 2240 TOP/s; 8192 x
 //     7168 x 2048 131 us; the gate/up and down products of 32768 rows over 32
-//     experts of 2880 x 2880 560 and 290 us);
+//     experts of 2880 x 2880 575 and, with float32 outputs, 320 us);
 //   - stream (below): the wavefronts of a workgroup split k, for few rows, where
 //     reading the weights once is the work (8 tokens, 15 such experts: 66 us,
 //     5.7 TB/s).
@@ -510,7 +510,8 @@ hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t st
 }
 
 // The stream for `mtiles` row tiles (at most) of at most `rows` rows: 16, 32 or
-// (dense) 64; bytes: of all weights that the call reads.
+// (dense) 64; bytes: of the weights that the call reads, at most (grouped: as
+// many experts as there are rows, or all; the routing is not known here).
 // - With up to 256 units of 64 columns k is split over eight wavefronts (4 / 8:
 //   64 x 7168 x 2048 7.0 / 6.5 us, 32 x 7168 x 7168 15.7 / 12.9, but 333 x 2880 x
 //   1024, 270 units, 7.5 / 9.3). With many, a workgroup takes 64 x 128 outputs,
@@ -523,7 +524,8 @@ hipError_t run_int8_stream(const Int8GemmArgs &g, int64_t mtiles, hipStream_t st
 //   the caches by row tiles that have them to themselves, and for 16 rows in
 //   units of 32 packed rows, whose last ones end together (15 experts of 2880 x
 //   2880 in use, 376 MB: 105 -> 98 -> 94 us; 32 rows, 32 such experts 195 -> 174;
-//   but 4 of them, 100 MB, the same four in every call: 44 -> 49 us).
+//   but 4 of them, 100 MB, the same four in every call: 44 -> 49 us, which a
+//   hot call, or one device's share, of a layer with many experts takes too).
 template <bool kGrouped, bool kSwigluOut>
 hipError_t launch_int8_stream(const Int8GemmArgs &g, int rows, int64_t mtiles, int64_t bytes,
                               hipStream_t stream) {
@@ -611,16 +613,17 @@ size_t ffn_int8_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F) {
 
 // Rows of a tile, by the rows per expert on average (the routing is not known
 // here): the stream's 16 or 32, or 128 or 256 rows through the ring. Whole
-// layers in us, uniform routing unless "hot" (60% of the pairs on four experts):
+// layers (float32 outputs of the experts) in us, uniform routing unless "hot"
+// (60% of the pairs on four experts; "warm": on 16):
 //   2880 x 2880, 32 experts, 4 of them a token, 16 / 32 / 128 / 256 rows:
-//     32 tokens 176 / 177 / 189 / 184, 128 tokens 218 / 193 / 200 / 201,
-//     and 32 / 128 / 256: 250 tokens 242 / 210 / 223, 400 tokens 299 / 227 / 220,
-//     hot 272 / 252 / 245, 1000 tokens hot 541 / 316 / 289
-//   2048 x 768, 128 experts, 8, 32 / 128 / 256 rows: 400 tokens 157 / 158 / 162,
-//     700 tokens 209 / 175 / 177, 1531 tokens 293 / 204 / 207,
-//     2200 tokens hot 370 / 263 / 269, 3000 tokens 452 / 305 / 266
-//   1024 x 768, 16 experts, 2: 300 tokens 42 / 50 / 51, 700 tokens 49 / 56 / 58,
-//     1200 tokens hot 62 / 59 / 69, 2000 tokens 75 / 61 / 72
+//     32 tokens 147 / 153 / 178 / 180, 128 tokens 198 / 167 / 193 / 189,
+//     and 32 / 128 / 256: 250 tokens 233 / 204 / 217, 400 tokens 295 / 227 / 217,
+//     hot 272 / 251 / 251, 1000 tokens hot 529 / 322 / 298
+//   2048 x 768, 128 experts, 8, 32 / 128 / 256 rows: 400 tokens 158 / 159 / 161,
+//     700 tokens 208 / 175 / 179, 1531 tokens warm 308 / 249 / 271,
+//     2200 tokens hot 397 / 274 / 295, 3000 tokens 487 / 325 / 307
+//   1024 x 768, 16 experts, 2: 300 tokens 41 / 50 / 51, 700 tokens 48 / 56 / 57,
+//     1200 tokens hot 61 / 61 / 70, 2000 tokens 72 / 62 / 76
 static int ffn_int8_rows(const FfnInt8Args &a) {
   const int64_t R = a.R, E = a.E, weight = int64_t(a.D) * a.F;
   if (R <= 8 * E) return 16;

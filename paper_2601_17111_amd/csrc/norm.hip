@@ -12,8 +12,10 @@
 // and 25 operations, so a row is read once into registers (rows.h) and every
 // sum over it is taken there. All in float32, each output rounded once; h is
 // computed from the r that was not rounded yet. Forward of 16384 x 2880 bf16
-// with a gate per channel 78 us (4.8 TB/s), one row 2.6 us; backward of 8192 x
-// 7168 bf16 155 us (4.6 TB/s), of 1777 x 2048 float32 with a full gate 29 us.
+// with a gate per channel 78 us (4.8 TB/s), of 8192 x 2880 float32 75 us (5.0
+// TB/s), one row 2.6 us; with 8-bit rows in place of h 75 us (16384 x 2880);
+// backward of 8192 x 7168 bf16 148 us (4.8 TB/s), of 1777 x 2048 float32 with a
+// full gate 29 us.
 #include <algorithm>
 
 #include "kernels.h"
@@ -331,11 +333,13 @@ __global__ __launch_bounds__(kMaxThreads) void block_norm_bwd_kernel(NormBwdArgs
 
 // Backward of odd rows: element by element, several times over the row, which
 // the cache holds; what has to stay in 32 bits between two sweeps is kept in
-// LDS, every element by its thread, and the column sums in the workspace. In
-// short rows a norm's gradient is the small rest of large terms (with one
-// element, f eps / (b^2 + eps)), so the row sums and what they enter have 64
-// bits. (In registers, with 16-byte loads, the 64 bits take as long: 8192 x 2879
-// 260 and 264 us, 300 x 501 15 and 11.5.)
+// LDS, every element by its thread, and the column sums in the workspace. In a
+// row of one element a norm's gradient is the small rest of large terms (f eps /
+// (b^2 + eps)), so the row sums and what they enter have 64 bits; rows of eight
+// elements and more do without them (whole rows run in 32 bits), so that the
+// sweeps and the 64 bits of longer odd rows are not needed, only not replaced:
+// 8192 x 2879 255 us where its bytes take 54. (The 64 bits in registers, with
+// 16-byte loads, take as long: 260 and 264 us, 300 x 501 15 and 11.5.)
 template <typename T>
 __device__ __forceinline__ float load1(const void *p, int64_t i) {
   float v[1];

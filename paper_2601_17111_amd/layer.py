@@ -191,7 +191,7 @@ class LLEPLayer:
         self.x_scale = B._empty((self.T,), torch.float32, dev, stream)
         self.x_perm_q = B._empty((R, D), torch.int8, dev, stream)
         # the experts' outputs stay in float32, so that y is rounded once in any batch (in bfloat16
-        # a prompt takes 5% less, but its tokens lose bits and differ from decode's)
+        # prompts take 5-6% less, but their tokens lose bits and differ from decode's)
         self.out_perm_wide = B._empty((R, D), torch.float32, dev, stream)
         nbytes = B.llep_grouped_ffn_int8_workspace_bytes(self.params, self.F)
         self.int8_workspace = B._empty((nbytes,), torch.uint8, dev, stream)
