@@ -523,6 +523,158 @@ int llep_combine_to_bf16(const llep_plan_params *params, const float *out_perm,
                          const int32_t *pair_row, const float *topk_gates,
                          int32_t D, void *y, hipStream_t stream);
 
+/* ---- routing ---------------------------------------------------------------
+ *
+ * Router logits to the expert ids and gates that the entry points above take.
+ * For every token, with logits l[e], e < E:
+ *   score  s[e] = softmax(l)[e] over all E, or sigmoid(l[e]);
+ *   key    what the choice goes by: l[e] itself or, where a bias is given or a
+ *          group's score is a sum, s[e] + bias[e] in float64, so that the choice
+ *          does not depend on how a score was rounded. The bias (of load
+ *          balancing, float32) is in the choice alone, not in the gates;
+ *   groups E experts are `groups` ranges of E / groups; a group's score is its
+ *          largest key or (LLEP_GROUP_TOP2) the sum of its two largest; only the
+ *          experts of the top_groups best groups remain;
+ *   ids    the K experts with the largest keys, in descending order;
+ *   gates  scale * s[id], or with `renormalize` scale * s[id] over the sum of
+ *          the chosen experts' scores (computed relative to the largest of them,
+ *          so that it holds however small they are).
+ * Ties, of experts and of groups, go to the lower index. An expert whose logit
+ * or bias is -infinity, or whose key is NaN, is not chosen (and not one of a
+ * group's two largest): where fewer than K remain, the last ids are -1 with
+ * gates of 0. llep_plan leaves such pairs out (and sets
+ * LLEP_STATUS_BAD_EXPERT_ID). Rows of -infinity alone, of padded tokens, are
+ * such rows. Gates are NaN where their formula is (a softmax over all experts,
+ * one of them NaN). */
+typedef enum { LLEP_SCORE_SOFTMAX = 0, LLEP_SCORE_SIGMOID = 1 } llep_score;
+typedef enum { LLEP_GROUP_MAX = 0, LLEP_GROUP_TOP2 = 1 } llep_group_score;
+#define LLEP_MAX_ROUTE_TOPK 64   /* largest K of the routing calls */
+#define LLEP_MAX_ROUTE_GROUPS 64 /* largest number of groups */
+
+/* Host memory, 40 bytes. */
+typedef struct {
+  int64_t T; /* >= 0; T * K < 2^31 */
+  int32_t K; /* in [1, LLEP_MAX_ROUTE_TOPK], at most E / groups * top_groups */
+  int32_t E; /* in [1, LLEP_MAX_EXPERTS] */
+  int32_t score;       /* llep_score */
+  int32_t groups;      /* in [1, LLEP_MAX_ROUTE_GROUPS], divides E; 1: none */
+  int32_t top_groups;  /* in [1, groups] */
+  int32_t group_score; /* llep_group_score */
+  int32_t renormalize; /* 0 or 1 */
+  float scale;         /* of the gates; finite and above 0 */
+} llep_route_params;
+
+/* logits [T][E] in dtype, bias [E] float32 or null, ids [T][K] int32, gates
+ * [T][K] float32; each aligned to its type. No workspace.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+int llep_route(const llep_route_params *params, llep_dtype dtype,
+               const void *logits, const float *bias, int32_t *ids,
+               float *gates, hipStream_t stream);
+
+/* d_logits [T][E] in dtype, all of it, from d_gates [T][K] and llep_route's
+ * logits, ids and gates (the choice has no gradient, so the bias has none).
+ * With g = gates, p = g / scale, e = ids[k], all in 32 bits and rounded once:
+ *   softmax, renormalized  d l[e] += g[k] (d g[k] - sum_j p[j] d g[j])
+ *   softmax                d l[e] += g[k] d g[k], and for every expert
+ *                          d l[e] -= s[e] sum_j g[j] d g[j]
+ *   sigmoid, renormalized  d l[e] += g[k] (1 - s[e]) (d g[k] - sum_j p[j] d g[j])
+ *   sigmoid                d l[e] += g[k] (1 - s[e]) d g[k]
+ * Ids outside [0, E) count for nothing, whatever their gates and d_gates are. An
+ * expert that a row names twice gets both, in the order of k. logits may be null
+ * for the renormalized softmax, which does not read it; bias, groups and
+ * group_score are not read. d_logits may be logits.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+int llep_route_backward(const llep_route_params *params, llep_dtype dtype,
+                        const void *logits, const int32_t *ids,
+                        const float *gates, const float *d_gates,
+                        void *d_logits, hipStream_t stream);
+
+/* ---- 4-bit floating point with shared exponents (MXFP4) ---------------------
+ *
+ * A row of D values is cut into blocks of 32 (the last may be shorter); a block
+ * has an exponent byte b and values v of 4 bits, standing for v 2^(b - 127). A
+ * value has its sign in bit 3 and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0..7) in the
+ * others; two lie in a byte, the first in its low half. b = 255: the whole block
+ * is NaN.
+ * In a "4-bit row" values and exponents are padded: llep_mxfp4_row_bytes(D)
+ * bytes of values (64 for every 128, the rest zeros) and
+ * llep_mxfp4_scale_bytes(D) bytes of exponents (16 for every 512; any but 255
+ * behind the last block). Both -1 for D outside [1, LLEP_MAX_FFN_DIM]. */
+int32_t llep_mxfp4_row_bytes(int32_t D);
+int32_t llep_mxfp4_scale_bytes(int32_t D);
+
+/* x [R][D] in dtype to 4-bit rows: q and scale, whose rows lie q_pitch and
+ * scale_pitch bytes apart (multiples of 16, at least the bytes above; a row's
+ * bytes beyond those are left as they are). b = max(floor(log2 max|x|) - 2 + 127,
+ * 1) over the block's values, which are rounded to the nearest of the grid, ties
+ * to the even code, 6 at most. A block with an infinity or a NaN gets b = 255.
+ * x is aligned to its type, q and scale to 16 bytes.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+int llep_quantize_rows_mxfp4(int64_t R, int32_t D, llep_dtype dtype,
+                             const void *x, uint8_t *q, int32_t q_pitch,
+                             uint8_t *scale, int32_t scale_pitch,
+                             hipStream_t stream);
+
+/* out [R][D] in dtype = what 4-bit rows stand for: exact, but that a result
+ * beyond the type's range is infinite. out is aligned to its type.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+int llep_dequantize_rows_mxfp4(int64_t R, int32_t D, llep_dtype dtype,
+                               const uint8_t *q, int32_t q_pitch,
+                               const uint8_t *scale, int32_t scale_pitch,
+                               void *out, hipStream_t stream);
+
+/* 4-bit weights for the products below, packed once: E matrices w [N][K], rows =
+ * output channels, of w_bytes bytes of values (at least K / 2, rounded up) and
+ * scale_bytes exponents (at least K / 32, rounded up) a row, one row after
+ * another: dense files' rows as well as 4-bit rows. With w_up and up_scale (both
+ * or none; N a multiple of 32) of gate and up rows together: packed as one matrix
+ * of 2 N rows, 32 gate rows and the matching 32 up rows by turns.
+ * llep_packed_mxfp4_bytes(E, N, K): bytes of E packed matrices (0 for sizes
+ * outside: E in [1, LLEP_MAX_EXPERTS], N in [1, LLEP_MAX_MXFP4_COLUMNS], K in [1,
+ * LLEP_MAX_FFN_DIM]); of gate and up rows, with 2 N. packed is 16-byte aligned.
+ * Errors: LLEP_E_ARG. */
+#define LLEP_MAX_MXFP4_COLUMNS (1 << 20)
+size_t llep_packed_mxfp4_bytes(int32_t E, int32_t N, int32_t K);
+int llep_pack_mxfp4(int32_t E, int32_t N, int32_t K, const uint8_t *w,
+                    const uint8_t *scale, const uint8_t *w_up,
+                    const uint8_t *up_scale, int32_t w_bytes,
+                    int32_t scale_bytes, uint8_t *packed, hipStream_t stream);
+
+/* out [M][N] in dtype = x w^T: x M 4-bit rows of K values (q_pitch and
+ * scale_pitch as above), w_packed one matrix of llep_pack_mxfp4. The products
+ * of a block are exact and summed in 32 bits, so are the blocks, and out is
+ * rounded once. The order of the sum depends on M, N and K, not on the
+ * values. x, x_scale, w_packed and out 16-byte aligned; M in [0,
+ * LLEP_MAX_MXFP4_ROWS]. No workspace.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE. */
+#define LLEP_MAX_MXFP4_ROWS 0x7fffff00
+int llep_mxfp4_matmul(int64_t M, int32_t N, int32_t K, const uint8_t *x,
+                      int32_t q_pitch, const uint8_t *x_scale,
+                      int32_t scale_pitch, const uint8_t *w_packed,
+                      llep_dtype dtype, void *out, hipStream_t stream);
+
+/* llep_grouped_ffn on 4-bit rows and weights: x_perm [T*K] rows of
+ * llep_mxfp4_row_bytes(D) bytes of values and, behind them,
+ * llep_mxfp4_scale_bytes(D) exponents (llep_permute moves such rows as half as
+ * many bfloat16); w_gate_up_packed E matrices of gate and up rows [F][D]
+ * together, w_down_packed E matrices [D][F]. The activation silu(g) u is computed
+ * in 32 bits and cut into 4-bit rows as by llep_quantize_rows_mxfp4. out_perm
+ * [T*K][D] in dtype (LLEP_F32: for llep_combine_to_bf16). D and F multiples of
+ * 64, at most LLEP_MAX_FFN_DIM. Rows of other devices than `device` (-1: all) and
+ * rows that no pair has are left as they are. Workspace of
+ * llep_grouped_ffn_mxfp4_workspace_bytes(params, F) bytes (0 for arguments
+ * outside their ranges), 256-byte aligned.
+ * Errors: LLEP_E_ARG, LLEP_E_DTYPE, LLEP_E_WORKSPACE. */
+size_t llep_grouped_ffn_mxfp4_workspace_bytes(const llep_plan_params *params,
+                                              int32_t F);
+int llep_grouped_ffn_mxfp4(const llep_plan_params *params,
+                           const llep_plan_buffers *plan, int32_t device,
+                           const uint8_t *x_perm,
+                           const uint8_t *w_gate_up_packed,
+                           const uint8_t *w_down_packed, int32_t D, int32_t F,
+                           llep_dtype dtype, void *out_perm, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
 /* One tensor of a list of gradients: n elements in dtype, dense. `data` and
  * `out` are device pointers; the array of descriptors is host memory, read
  * during the call only. */

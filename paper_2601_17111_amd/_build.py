@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(PKG, "libllep.so")
 
 SOURCES = ["plan.hip", "permute.hip", "pack.hip", "stream_ffn.hip", "grouped_ffn.hip",
            "grouped_ffn_bwd.hip", "ffn_f32.hip", "norm.hip", "clip.hip",
-           "int8.hip", "abi.cpp"]
+           "int8.hip", "mxfp4.hip", "route.hip", "abi.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -32,6 +32,10 @@ LLEP_MAX_DEVICES = 64
 LLEP_MAX_FFN_DIM = 65536
 LLEP_MAX_NORM_DIM = 8192
 LLEP_GATE_NONE, LLEP_GATE_CHANNEL, LLEP_GATE_TOKEN, LLEP_GATE_FULL = range(4)
+LLEP_SCORE_SOFTMAX, LLEP_SCORE_SIGMOID = range(2)
+LLEP_GROUP_MAX, LLEP_GROUP_TOP2 = range(2)
+LLEP_MAX_ROUTE_TOPK = 64
+LLEP_MAX_ROUTE_GROUPS = 64
 
 EXPORTED = [
     "llep_plan", "llep_permute", "llep_grouped_ffn", "llep_combine",
@@ -47,6 +51,10 @@ EXPORTED = [
     "llep_int8_matmul_workspace_bytes", "llep_int8_matmul",
     "llep_grouped_ffn_int8_workspace_bytes", "llep_grouped_ffn_int8",
     "llep_grouped_ffn_int8_f32", "llep_combine_to_bf16",
+    "llep_route", "llep_route_backward", "llep_mxfp4_row_bytes", "llep_mxfp4_scale_bytes",
+    "llep_quantize_rows_mxfp4", "llep_dequantize_rows_mxfp4", "llep_packed_mxfp4_bytes",
+    "llep_pack_mxfp4", "llep_mxfp4_matmul", "llep_grouped_ffn_mxfp4_workspace_bytes",
+    "llep_grouped_ffn_mxfp4",
 ]
 LLEP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -81,6 +89,12 @@ class llep_gradient(ctypes.Structure):
 _DTYPE_OF, _IS_CUDA = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
 
 
+class llep_route_params(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("K", "E", "score", "groups", "top_groups", "group_score",
+                                      "renormalize")] + [("scale", ctypes.c_float)]
+
+
 class LLEPError(RuntimeError):
     def __init__(self, code: int, where: str, msg: str):
         super().__init__(f"{where} failed with code {code}: {msg}")
@@ -101,6 +115,7 @@ def lib() -> ctypes.CDLL:
         pp = ctypes.POINTER(llep_plan_params)
         pb = ctypes.POINTER(llep_plan_buffers)
         pg = ctypes.POINTER(llep_gradient)
+        pr = ctypes.POINTER(llep_route_params)
         i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         f32 = ctypes.c_float
         sigs = {
@@ -149,6 +164,21 @@ def lib() -> ctypes.CDLL:
             "llep_grouped_ffn_int8_f32": (ctypes.c_int, [pp, pb, i32, _P, _P, _P, _P, _P, _P, _P,
                                                          _P, i32, i32, _P, _P, sz, _P]),
             "llep_combine_to_bf16": (ctypes.c_int, [pp, _P, _P, _P, i32, _P, _P]),
+            "llep_route": (ctypes.c_int, [pr, ctypes.c_int, _P, _P, _P, _P, _P]),
+            "llep_route_backward": (ctypes.c_int, [pr, ctypes.c_int, _P, _P, _P, _P, _P, _P]),
+            "llep_mxfp4_row_bytes": (i32, [i32]),
+            "llep_mxfp4_scale_bytes": (i32, [i32]),
+            "llep_quantize_rows_mxfp4": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, _P, i32, _P,
+                                                        i32, _P]),
+            "llep_dequantize_rows_mxfp4": (ctypes.c_int, [i64, i32, ctypes.c_int, _P, i32, _P,
+                                                          i32, _P, _P]),
+            "llep_packed_mxfp4_bytes": (sz, [i32, i32, i32]),
+            "llep_pack_mxfp4": (ctypes.c_int, [i32, i32, i32, _P, _P, _P, _P, i32, i32, _P, _P]),
+            "llep_mxfp4_matmul": (ctypes.c_int, [i64, i32, i32, _P, i32, _P, i32, _P,
+                                                 ctypes.c_int, _P, _P]),
+            "llep_grouped_ffn_mxfp4_workspace_bytes": (sz, [pp, i32]),
+            "llep_grouped_ffn_mxfp4": (ctypes.c_int, [pp, pb, i32, _P, _P, _P, i32, i32,
+                                                      ctypes.c_int, _P, _P, sz, _P]),
             "llep_clip_gradients_workspace_bytes": (sz, []),
             "llep_gradient_norm": (ctypes.c_int, [i32, pg, _P, _P, sz, _P]),
             "llep_clip_gradients": (ctypes.c_int, [i32, pg, f32, _P, _P, sz, _P]),
@@ -692,3 +722,197 @@ def llep_combine_to_bf16(params: llep_plan_params, out_perm, pair_row, topk_gate
     _check(lib().llep_combine_to_bf16(ctypes.byref(params), _ptr(out_perm), _ptr(pair_row),
                                       _ptr(topk_gates), D, _ptr(y), _stream(stream)),
            "llep_combine_to_bf16")
+
+
+# ---- routing -----------------------------------------------------------------------
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, whose stream a call goes to."""
+    import torch
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"a tensor is on {t.device}, the current device is {current}")
+
+
+def make_route(T: int, K: int, E: int, score: str = "softmax", groups: int = 1,
+               top_groups: int = 1, group_score: str = "max", renormalize: bool = True,
+               scale: float = 1.0) -> llep_route_params:
+    """Parameters of llep_route (see llep.h). score: "softmax" or "sigmoid"; group_score: "max" or
+    "top2"."""
+    scores = {"softmax": LLEP_SCORE_SOFTMAX, "sigmoid": LLEP_SCORE_SIGMOID}
+    kinds = {"max": LLEP_GROUP_MAX, "top2": LLEP_GROUP_TOP2}
+    if score not in scores:
+        raise ValueError(f"score is {score!r}, not 'softmax' or 'sigmoid'")
+    if group_score not in kinds:
+        raise ValueError(f"group_score is {group_score!r}, not 'max' or 'top2'")
+    return llep_route_params(T=T, K=K, E=E, score=scores[score], groups=groups,
+                             top_groups=top_groups, group_score=kinds[group_score],
+                             renormalize=int(bool(renormalize)), scale=scale)
+
+
+def llep_route(params: llep_route_params, logits, bias, ids, gates, stream=None):
+    """Router logits [T, E] (bf16 or float32) to ids [T, K] int32 and gates [T, K] float32 (see
+    llep.h); bias [E] float32 or None."""
+    import torch
+    T, K, E = params.T, params.K, params.E
+    code = _dtype_code(logits)
+    _dense("logits", logits, (T, E), logits.dtype)
+    _dense("bias", bias, (E,), torch.float32)
+    _dense("ids", ids, (T, K), torch.int32)
+    _dense("gates", gates, (T, K), torch.float32)
+    _here(logits, bias, ids, gates)
+    _check(lib().llep_route(ctypes.byref(params), code, _ptr(logits), _ptr(bias), _ptr(ids),
+                            _ptr(gates), _stream(stream)), "llep_route")
+
+
+def llep_route_backward(params: llep_route_params, logits, ids, gates, d_gates, d_logits,
+                        stream=None):
+    """d_logits [T, E] (bf16 or float32) from d_gates [T, K] float32 and llep_route's inputs and
+    outputs; logits (of d_logits' type) may be None for the renormalized softmax."""
+    import torch
+    T, K, E = params.T, params.K, params.E
+    code = _dtype_code(d_logits)
+    _dense("logits", logits, (T, E), d_logits.dtype)
+    _dense("ids", ids, (T, K), torch.int32)
+    _dense("gates", gates, (T, K), torch.float32)
+    _dense("d_gates", d_gates, (T, K), torch.float32)
+    _dense("d_logits", d_logits, (T, E), d_logits.dtype)
+    _here(logits, ids, gates, d_gates, d_logits)
+    _check(lib().llep_route_backward(ctypes.byref(params), code, _ptr(logits), _ptr(ids),
+                                     _ptr(gates), _ptr(d_gates), _ptr(d_logits),
+                                     _stream(stream)), "llep_route_backward")
+
+
+# ---- 4-bit rows and products ---------------------------------------------------------
+
+def llep_mxfp4_row_bytes(D: int) -> int:
+    """Bytes of the values of a 4-bit row of D values."""
+    n = lib().llep_mxfp4_row_bytes(D)
+    if n < 0:
+        raise LLEPError(LLEP_E_ARG, "llep_mxfp4_row_bytes", "D outside [1, LLEP_MAX_FFN_DIM]")
+    return n
+
+
+def llep_mxfp4_scale_bytes(D: int) -> int:
+    """Bytes of the exponents of a 4-bit row of D values."""
+    n = lib().llep_mxfp4_scale_bytes(D)
+    if n < 0:
+        raise LLEPError(LLEP_E_ARG, "llep_mxfp4_scale_bytes", "D outside [1, LLEP_MAX_FFN_DIM]")
+    return n
+
+
+def _byte_rows(what: str, t, R: int, least: int) -> int:
+    """The bytes from one row of t to the next: t [R, >= least] uint8 on the GPU, whose rows may be
+    parts of longer ones (a view of a buffer's columns)."""
+    import torch
+    if t.dtype is not torch.uint8:
+        raise TypeError(f"{what} is {t.dtype}, not {torch.uint8}")
+    if t.dim() != 2 or t.shape[0] != R or t.shape[1] < least:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not [{R}, {least}] or wider")
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on a GPU")
+    if R <= 1:  # the stride of an only row means nothing
+        return (t.shape[1] + 15) // 16 * 16
+    if t.stride(1) != 1 or t.stride(0) < t.shape[1]:
+        raise ValueError(f"{what} is not made of rows of bytes")
+    return t.stride(0)
+
+
+def llep_quantize_rows_mxfp4(x, q, scale, stream=None):
+    """x [R, D] (bf16 or float32) to 4-bit rows: q [R, llep_mxfp4_row_bytes(D)] and scale [R,
+    llep_mxfp4_scale_bytes(D)] uint8 (rows a multiple of 16 bytes apart)."""
+    R, D = x.shape
+    code = _dtype_code(x)
+    _dense("x", x, (R, D), x.dtype)
+    q_pitch = _byte_rows("q", q, R, llep_mxfp4_row_bytes(D))
+    s_pitch = _byte_rows("scale", scale, R, llep_mxfp4_scale_bytes(D))
+    _here(x, q, scale)
+    _check(lib().llep_quantize_rows_mxfp4(R, D, code, _ptr(x), _ptr(q), q_pitch, _ptr(scale),
+                                          s_pitch, _stream(stream)), "llep_quantize_rows_mxfp4")
+
+
+def llep_dequantize_rows_mxfp4(q, scale, out, stream=None):
+    """out [R, D] (bf16 or float32) = what the 4-bit rows q, scale stand for."""
+    R, D = out.shape
+    code = _dtype_code(out)
+    _dense("out", out, (R, D), out.dtype)
+    q_pitch = _byte_rows("q", q, R, llep_mxfp4_row_bytes(D))
+    s_pitch = _byte_rows("scale", scale, R, llep_mxfp4_scale_bytes(D))
+    _here(q, scale, out)
+    _check(lib().llep_dequantize_rows_mxfp4(R, D, code, _ptr(q), q_pitch, _ptr(scale), s_pitch,
+                                            _ptr(out), _stream(stream)),
+           "llep_dequantize_rows_mxfp4")
+
+
+def llep_pack_matrix_mxfp4(w, scale, w_up=None, up_scale=None, K: int = None, stream=None):
+    """Packed copy of 4-bit weights: w [N, bytes] or [E, N, bytes] uint8 (two values a byte), rows
+    = output channels, with exponents scale [.., N, blocks] uint8; with w_up and up_scale (the same
+    shapes) of gate and up rows together. K: values of a row (2 * bytes, where it is not given).
+    Returns a uint8 tensor [E, bytes]."""
+    import torch
+    if w.dim() not in (2, 3):
+        raise ValueError("weights are [N, bytes] or [E, N, bytes]")
+    E, N, w_bytes = (1, *w.shape) if w.dim() == 2 else w.shape
+    if K is None:
+        K = 2 * w_bytes
+    if w_bytes < (K + 1) // 2 or scale.shape[-1] < (K + 31) // 32:
+        raise ValueError(f"rows of {w_bytes} bytes and {scale.shape[-1]} exponents hold no {K} values")
+    _dense("w", w, w.shape, torch.uint8)
+    _dense("scale", scale, (*w.shape[:-1], scale.shape[-1]), torch.uint8)
+    if (w_up is None) != (up_scale is None):
+        raise ValueError("w_up and up_scale: both or none")
+    _dense("w_up", w_up, w.shape, torch.uint8)
+    _dense("up_scale", up_scale, scale.shape, torch.uint8)
+    _here(w, scale, w_up, up_scale)
+    nbytes = lib().llep_packed_mxfp4_bytes(E, N if w_up is None else 2 * N, K)
+    if nbytes == 0:
+        raise LLEPError(LLEP_E_ARG, "llep_pack_matrix_mxfp4", "E, N or K outside its range")
+    out = _empty((E, nbytes // E), torch.uint8, w.device, stream)
+    _check(lib().llep_pack_mxfp4(E, N, K, _ptr(w), _ptr(scale), _ptr(w_up), _ptr(up_scale),
+                                 w_bytes, scale.shape[-1], _ptr(out), _stream(stream)),
+           "llep_pack_mxfp4")
+    return out
+
+
+def llep_mxfp4_matmul(x, x_scale, w_packed, out, K: int, stream=None):
+    """out [M, N] (bf16 or float32) = x w^T: x, x_scale 4-bit rows of K values
+    (llep_quantize_rows_mxfp4), w_packed one matrix of llep_pack_matrix_mxfp4."""
+    import torch
+    M, N = out.shape
+    code = _dtype_code(out)
+    q_pitch = _byte_rows("x", x, M, llep_mxfp4_row_bytes(K))
+    s_pitch = _byte_rows("x_scale", x_scale, M, llep_mxfp4_scale_bytes(K))
+    _dense("w_packed", w_packed, (1, lib().llep_packed_mxfp4_bytes(1, N, K)), torch.uint8)
+    _dense("out", out, (M, N), out.dtype)
+    _here(x, x_scale, w_packed, out)
+    _check(lib().llep_mxfp4_matmul(M, N, K, _ptr(x), q_pitch, _ptr(x_scale), s_pitch,
+                                   _ptr(w_packed), code, _ptr(out), _stream(stream)),
+           "llep_mxfp4_matmul")
+
+
+def llep_grouped_ffn_mxfp4_workspace_bytes(params: llep_plan_params, F: int) -> int:
+    return lib().llep_grouped_ffn_mxfp4_workspace_bytes(ctypes.byref(params), F)
+
+
+def llep_grouped_ffn_mxfp4(params: llep_plan_params, bufs: PlanBuffers, device: int, x_perm,
+                           w_gate_up, w_down, D: int, F: int, out_perm, workspace, stream=None):
+    """The grouped FFN on 4-bit rows and weights (see llep.h): x_perm [T*K, bytes] uint8, values
+    and then exponents of each row (llep_mxfp4_row_bytes(D) + llep_mxfp4_scale_bytes(D) bytes);
+    weights from llep_pack_matrix_mxfp4; out_perm [T*K, D] bf16 or float32."""
+    import torch
+    R, E = params.T * params.K, params.E
+    if x_perm.shape[0] < R or out_perm.shape[0] < R:
+        raise ValueError("x_perm and out_perm need T * K rows")
+    code = _dtype_code(out_perm)
+    _dense("x_perm", x_perm,
+           (x_perm.shape[0], llep_mxfp4_row_bytes(D) + llep_mxfp4_scale_bytes(D)), torch.uint8)
+    L = lib()
+    for what, t, n, k in (("w_gate_up", w_gate_up, 2 * F, D), ("w_down", w_down, D, F)):
+        _dense(what, t, (E, L.llep_packed_mxfp4_bytes(1, n, k)), torch.uint8)
+    _dense("out_perm", out_perm, (out_perm.shape[0], D), out_perm.dtype)
+    _here(x_perm, w_gate_up, w_down, out_perm, workspace)
+    _check(L.llep_grouped_ffn_mxfp4(
+        ctypes.byref(params), ctypes.byref(bufs.struct), device, _ptr(x_perm), _ptr(w_gate_up),
+        _ptr(w_down), D, F, code, _ptr(out_perm), *_workspace(workspace), _stream(stream)),
+        "llep_grouped_ffn_mxfp4")

@@ -119,6 +119,63 @@ int check_gradients(int32_t n, const llep_gradient *grads, bool scale, const flo
   return LLEP_OK;
 }
 
+int check_route(const llep_route_params *p, llep_dtype dtype) {
+  if (!p) return fail(LLEP_E_ARG, "params is null");
+  if (elem_bytes(dtype) == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  if (p->T < 0) return fail(LLEP_E_ARG, "T < 0");
+  if (p->E < 1 || p->E > LLEP_MAX_EXPERTS) return fail(LLEP_E_ARG, "E outside [1, LLEP_MAX_EXPERTS]");
+  if (p->K < 1 || p->K > LLEP_MAX_ROUTE_TOPK)
+    return fail(LLEP_E_ARG, "K outside [1, LLEP_MAX_ROUTE_TOPK]");
+  if (p->T > int64_t(INT32_MAX) / p->K) return fail(LLEP_E_ARG, "T * K >= 2^31");
+  if (p->score != LLEP_SCORE_SOFTMAX && p->score != LLEP_SCORE_SIGMOID)
+    return fail(LLEP_E_ARG, "unknown score");
+  if (p->groups < 1 || p->groups > LLEP_MAX_ROUTE_GROUPS || p->E % p->groups != 0)
+    return fail(LLEP_E_ARG, "groups must divide E and be in [1, LLEP_MAX_ROUTE_GROUPS]");
+  if (p->top_groups < 1 || p->top_groups > p->groups)
+    return fail(LLEP_E_ARG, "top_groups outside [1, groups]");
+  if (p->K > p->E / p->groups * p->top_groups)
+    return fail(LLEP_E_ARG, "K is more than the experts of top_groups groups");
+  if (p->group_score != LLEP_GROUP_MAX && p->group_score != LLEP_GROUP_TOP2)
+    return fail(LLEP_E_ARG, "unknown group score");
+  if (p->renormalize != 0 && p->renormalize != 1) return fail(LLEP_E_ARG, "renormalize is 0 or 1");
+  if (!(p->scale > 0.0f) || p->scale > 3.4028234e38f)
+    return fail(LLEP_E_ARG, "scale must be finite and above 0");
+  return LLEP_OK;
+}
+
+llep::RouteArgs route_args(const llep_route_params *p, llep_dtype dtype) {
+  llep::RouteArgs a = {};
+  a.T = p->T;
+  a.K = p->K;
+  a.E = p->E;
+  a.groups = p->top_groups < p->groups ? p->groups : 1;  // all of them: no choice
+  a.top_groups = p->top_groups;
+  a.score = p->score;
+  a.group_score = p->group_score;
+  a.renormalize = p->renormalize != 0;
+  a.scale = p->scale;
+  a.dtype = dtype;
+  return a;
+}
+
+// 4-bit rows of K values that a call reads or writes
+int check_mxfp4_rows(int64_t R, int32_t K, const uint8_t *q, int32_t q_pitch, const uint8_t *scale,
+                     int32_t scale_pitch) {
+  if (R < 0) return fail(LLEP_E_ARG, "fewer than 0 rows");
+  if (K < 1 || K > LLEP_MAX_FFN_DIM)
+    return fail(LLEP_E_ARG, "values of a row outside [1, LLEP_MAX_FFN_DIM]");
+  if (q_pitch % 16 != 0 || q_pitch < llep::mxfp4_row_bytes(K) || q_pitch > LLEP_MAX_FFN_DIM)
+    return fail(LLEP_E_ARG, "q_pitch must be a multiple of 16 from llep_mxfp4_row_bytes on, at most "
+                            "LLEP_MAX_FFN_DIM");
+  if (scale_pitch % 16 != 0 || scale_pitch < llep::mxfp4_scale_bytes(K) ||
+      scale_pitch > LLEP_MAX_FFN_DIM)
+    return fail(LLEP_E_ARG, "scale_pitch must be a multiple of 16 from llep_mxfp4_scale_bytes on, at "
+                            "most LLEP_MAX_FFN_DIM");
+  if (R > 0 && (!q || !scale)) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned16(q) || !aligned16(scale)) return fail(LLEP_E_ARG, "4-bit rows not 16-byte aligned");
+  return LLEP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -736,6 +793,171 @@ int llep_grouped_ffn_int8_f32(const llep_plan_params *params, const llep_plan_bu
   return grouped_ffn_int8(params, plan, device, x_perm, x_scale, row_pair, w_gate_up_packed,
                           gate_scale, up_scale, w_down_packed, down_scale, D, F, out_perm, true,
                           workspace, workspace_bytes, stream, "llep_grouped_ffn_int8_f32");
+}
+
+int llep_route(const llep_route_params *params, llep_dtype dtype, const void *logits,
+               const float *bias, int32_t *ids, float *gates, hipStream_t stream) {
+  const int rc = check_route(params, dtype);
+  if (rc != LLEP_OK) return rc;
+  if (params->T > 0 && (!logits || !ids || !gates)) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned_to(logits, elem_bytes(dtype)) || !aligned_to(bias, 4) || !aligned_to(ids, 4) ||
+      !aligned_to(gates, 4))
+    return fail(LLEP_E_ARG, "data not aligned to its type");
+  llep::RouteArgs a = route_args(params, dtype);
+  a.logits = logits;
+  a.bias = bias;
+  a.ids = ids;
+  a.gates = gates;
+  return hip_result(llep::launch_route(a, false, stream), "llep_route");
+}
+
+int llep_route_backward(const llep_route_params *params, llep_dtype dtype, const void *logits,
+                        const int32_t *ids, const float *gates, const float *d_gates,
+                        void *d_logits, hipStream_t stream) {
+  const int rc = check_route(params, dtype);
+  if (rc != LLEP_OK) return rc;
+  const bool reads = params->score != LLEP_SCORE_SOFTMAX || !params->renormalize;
+  if (params->T > 0 && ((reads && !logits) || !ids || !gates || !d_gates || !d_logits))
+    return fail(LLEP_E_ARG, "a data pointer is null");
+  const size_t eb = elem_bytes(dtype);
+  if (!aligned_to(logits, eb) || !aligned_to(d_logits, eb) || !aligned_to(ids, 4) ||
+      !aligned_to(gates, 4) || !aligned_to(d_gates, 4))
+    return fail(LLEP_E_ARG, "data not aligned to its type");
+  llep::RouteArgs a = route_args(params, dtype);
+  a.logits = logits;
+  a.ids = const_cast<int32_t *>(ids);
+  a.gates = const_cast<float *>(gates);
+  a.d_gates = d_gates;
+  a.d_logits = d_logits;
+  return hip_result(llep::launch_route(a, true, stream), "llep_route_backward");
+}
+
+int32_t llep_mxfp4_row_bytes(int32_t D) {
+  return D < 1 || D > LLEP_MAX_FFN_DIM ? -1 : llep::mxfp4_row_bytes(D);
+}
+
+int32_t llep_mxfp4_scale_bytes(int32_t D) {
+  return D < 1 || D > LLEP_MAX_FFN_DIM ? -1 : llep::mxfp4_scale_bytes(D);
+}
+
+int llep_quantize_rows_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const void *x, uint8_t *q,
+                             int32_t q_pitch, uint8_t *scale, int32_t scale_pitch,
+                             hipStream_t stream) {
+  const size_t eb = elem_bytes(dtype);
+  if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  const int rc = check_mxfp4_rows(R, D, q, q_pitch, scale, scale_pitch);
+  if (rc != LLEP_OK) return rc;
+  if (R > 0 && !x) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned_to(x, eb)) return fail(LLEP_E_ARG, "x not aligned to its type");
+  return hip_result(
+      llep::launch_quantize_mxfp4(R, D, dtype, x, q, q_pitch, scale, scale_pitch, stream),
+      "llep_quantize_rows_mxfp4");
+}
+
+int llep_dequantize_rows_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const uint8_t *q,
+                               int32_t q_pitch, const uint8_t *scale, int32_t scale_pitch,
+                               void *out, hipStream_t stream) {
+  const size_t eb = elem_bytes(dtype);
+  if (eb == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  const int rc = check_mxfp4_rows(R, D, q, q_pitch, scale, scale_pitch);
+  if (rc != LLEP_OK) return rc;
+  if (R > 0 && !out) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned_to(out, eb)) return fail(LLEP_E_ARG, "out not aligned to its type");
+  return hip_result(
+      llep::launch_dequantize_mxfp4(R, D, dtype, q, q_pitch, scale, scale_pitch, out, stream),
+      "llep_dequantize_rows_mxfp4");
+}
+
+size_t llep_packed_mxfp4_bytes(int32_t E, int32_t N, int32_t K) {
+  if (E < 1 || E > LLEP_MAX_EXPERTS || N < 1 || N > LLEP_MAX_MXFP4_COLUMNS || K < 1 ||
+      K > LLEP_MAX_FFN_DIM)
+    return 0;
+  return size_t(E) * llep::packed_mxfp4_bytes(N, K);
+}
+
+int llep_pack_mxfp4(int32_t E, int32_t N, int32_t K, const uint8_t *w, const uint8_t *scale,
+                    const uint8_t *w_up, const uint8_t *up_scale, int32_t w_bytes,
+                    int32_t scale_bytes, uint8_t *packed, hipStream_t stream) {
+  if (llep_packed_mxfp4_bytes(E, N, K) == 0) return fail(LLEP_E_ARG, "E, N or K outside its range");
+  if ((w_up != nullptr) != (up_scale != nullptr))
+    return fail(LLEP_E_ARG, "w_up and up_scale: both or none");
+  if (w_up && (N % 32 != 0 || N > LLEP_MAX_FFN_DIM))
+    return fail(LLEP_E_ARG, "gate and up rows: N must be a multiple of 32, at most LLEP_MAX_FFN_DIM");
+  if (w_bytes < (K + 1) / 2 || scale_bytes < (K + 31) / 32)
+    return fail(LLEP_E_ARG, "w_bytes or scale_bytes below those of K values");
+  if (!w || !scale || !packed) return fail(LLEP_E_ARG, "a weight pointer is null");
+  if (!aligned16(packed)) return fail(LLEP_E_ARG, "packed weights not 16-byte aligned");
+  return hip_result(llep::launch_pack_mxfp4(E, N, K, w, scale, w_up, up_scale, w_bytes, scale_bytes,
+                                            packed, stream),
+                    "llep_pack_mxfp4");
+}
+
+int llep_mxfp4_matmul(int64_t M, int32_t N, int32_t K, const uint8_t *x, int32_t q_pitch,
+                      const uint8_t *x_scale, int32_t scale_pitch, const uint8_t *w_packed,
+                      llep_dtype dtype, void *out, hipStream_t stream) {
+  if (elem_bytes(dtype) == 0) return fail(LLEP_E_DTYPE, "unknown dtype");
+  if (llep_packed_mxfp4_bytes(1, N, K) == 0) return fail(LLEP_E_ARG, "N or K outside its range");
+  if (M > LLEP_MAX_MXFP4_ROWS) return fail(LLEP_E_ARG, "M above LLEP_MAX_MXFP4_ROWS");
+  const int rc = check_mxfp4_rows(M, K, x, q_pitch, x_scale, scale_pitch);
+  if (rc != LLEP_OK) return rc;
+  if (!w_packed || (M > 0 && !out)) return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned16(w_packed) || !aligned16(out)) return fail(LLEP_E_ARG, "data not 16-byte aligned");
+  llep::MxMatmulArgs a = {};
+  a.M = M;
+  a.N = N;
+  a.K = K;
+  a.x_pitch = q_pitch;
+  a.s_pitch = scale_pitch;
+  a.dtype = dtype;
+  a.x = x;
+  a.x_scale = x_scale;
+  a.w = w_packed;
+  a.out = out;
+  return hip_result(llep::launch_mxfp4_matmul(a, stream), "llep_mxfp4_matmul");
+}
+
+size_t llep_grouped_ffn_mxfp4_workspace_bytes(const llep_plan_params *params, int32_t F) {
+  if (check_params(params) != LLEP_OK || F < 1 || F > LLEP_MAX_FFN_DIM) return 0;
+  return llep::ffn_mxfp4_workspace_bytes(params->T * params->K, params->E, params->P, F);
+}
+
+int llep_grouped_ffn_mxfp4(const llep_plan_params *params, const llep_plan_buffers *plan,
+                           int32_t device, const uint8_t *x_perm, const uint8_t *w_gate_up_packed,
+                           const uint8_t *w_down_packed, int32_t D, int32_t F, llep_dtype dtype,
+                           void *out_perm, void *workspace, size_t workspace_bytes,
+                           hipStream_t stream) {
+  int rc = check_params(params);
+  if (rc != LLEP_OK) return rc;
+  if ((rc = check_plan_buffers(plan)) != LLEP_OK) return rc;
+  if ((rc = check_ffn_dims(D, F, dtype)) != LLEP_OK) return rc;
+  if (device < -1 || device >= params->P) return fail(LLEP_E_ARG, "device outside [-1, P)");
+  // (arrays of no rows may have no address)
+  if (!w_gate_up_packed || !w_down_packed || (params->T > 0 && (!x_perm || !out_perm)))
+    return fail(LLEP_E_ARG, "a data pointer is null");
+  if (!aligned16(x_perm) || !aligned16(w_gate_up_packed) || !aligned16(w_down_packed) ||
+      !aligned16(out_perm))
+    return fail(LLEP_E_ARG, "data not 16-byte aligned");
+  const size_t need = llep_grouped_ffn_mxfp4_workspace_bytes(params, F);
+  if (!workspace || workspace_bytes < need)
+    return fail(LLEP_E_WORKSPACE,
+                "workspace missing or smaller than llep_grouped_ffn_mxfp4_workspace_bytes");
+  if (!aligned_to(workspace, 256)) return fail(LLEP_E_WORKSPACE, "workspace not 256-byte aligned");
+  llep::FfnMxArgs a = {};
+  a.R = params->T * params->K;
+  a.P = params->P;
+  a.E = params->E;
+  a.D = D;
+  a.F = F;
+  a.device = device;
+  a.groups = plan->groups;
+  a.group_begin = plan->group_begin;
+  a.x_perm = x_perm;
+  a.w_gate_up = w_gate_up_packed;
+  a.w_down = w_down_packed;
+  a.out_perm = out_perm;
+  a.f32_out = dtype == LLEP_F32;
+  a.ws = workspace;
+  return hip_result(llep::launch_ffn_mxfp4(a, stream), "llep_grouped_ffn_mxfp4");
 }
 
 }  // extern "C"

@@ -188,6 +188,55 @@ hipError_t launch_tile_table(const int32_t *groups, const int32_t *group_begin, 
                              int32_t device, int32_t P, int32_t BM, int4 *tiles, int32_t *n_tiles,
                              hipStream_t stream);
 
+// Routing and its gradient (route.hip): llep_route's arguments; backward reads
+// ids and gates.
+struct RouteArgs {
+  int64_t T;
+  int32_t K, E, groups, top_groups, score, group_score;
+  bool renormalize;
+  float scale;
+  llep_dtype dtype;  // of logits and d_logits
+  const void *logits;
+  const float *bias, *d_gates;
+  int32_t *ids;
+  float *gates;
+  void *d_logits;
+};
+hipError_t launch_route(const RouteArgs &a, bool backward, hipStream_t stream);
+
+// 4-bit rows and products (mxfp4.hip).
+int32_t mxfp4_row_bytes(int32_t K);
+int32_t mxfp4_scale_bytes(int32_t K);
+hipError_t launch_quantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const void *x, uint8_t *q,
+                                 int32_t q_pitch, uint8_t *scale, int32_t s_pitch,
+                                 hipStream_t stream);
+hipError_t launch_dequantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const uint8_t *q,
+                                   int32_t q_pitch, const uint8_t *scale, int32_t s_pitch,
+                                   void *out, hipStream_t stream);
+size_t packed_mxfp4_bytes(int32_t N, int32_t K);  // of one expert
+// w1, s1: null, or the up weights whose rows alternate with those of w0 by 32
+hipError_t launch_pack_mxfp4(int32_t E, int32_t N, int32_t K, const uint8_t *w0, const uint8_t *s0,
+                             const uint8_t *w1, const uint8_t *s1, int32_t w_bytes,
+                             int32_t s_bytes, uint8_t *out, hipStream_t stream);
+struct MxMatmulArgs {
+  int64_t M;
+  int32_t N, K, x_pitch, s_pitch;
+  llep_dtype dtype;  // of out
+  const uint8_t *x, *x_scale, *w;
+  void *out;
+};
+hipError_t launch_mxfp4_matmul(const MxMatmulArgs &a, hipStream_t stream);
+struct FfnMxArgs {
+  int64_t R;
+  int32_t P, E, D, F, device;
+  const int32_t *groups, *group_begin;
+  const uint8_t *x_perm, *w_gate_up, *w_down;
+  void *out_perm, *ws;
+  bool f32_out;  // out_perm is float32, else bfloat16
+};
+size_t ffn_mxfp4_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F);
+hipError_t launch_ffn_mxfp4(const FfnMxArgs &a, hipStream_t stream);
+
 // Gradient norm and clipping (clip.hip).
 struct ClipArgs {
   int32_t n;

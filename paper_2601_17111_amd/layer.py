@@ -65,6 +65,83 @@ class Int8Experts:
             return cls(*parts)
 
 
+class Mxfp4Experts:
+    """Expert weights in 4-bit floating point for LLEPLayer.forward_mxfp4, packed once.
+
+    w_gate, w_up [E, F, D / 2] and w_down [E, D, F / 2] uint8, rows = output channels, two values a
+    byte, with an exponent byte for every 32 values: [E, F, D / 32] (twice) and [E, D, F / 32]; D
+    and F multiples of 64. The form of MXFP4 files, and (rows may be longer) of
+    llep_quantize_rows_mxfp4 on the transposed weights; D and F are given for those.
+    """
+
+    def __init__(self, w_gate, gate_scale, w_up, up_scale, w_down, down_scale, D: int = None,
+                 F: int = None, stream=None):
+        if w_gate.dim() != 3 or w_down.dim() != 3:
+            raise ValueError("w_gate and w_up are [E, F, D / 2], w_down is [E, D, F / 2]")
+        E = w_gate.shape[0]
+        D = 2 * w_gate.shape[2] if D is None else D
+        F = w_gate.shape[1] if F is None else F
+        if (w_gate.shape[1] != F or w_up.shape != w_gate.shape or up_scale.shape != gate_scale.shape
+                or tuple(w_down.shape[:2]) != (E, D)):
+            raise ValueError("w_gate and w_up are [E, F, D / 2], w_down is [E, D, F / 2], with "
+                             "exponents for every 32 values")
+        if D % 64 or F % 64 or not 0 < D <= B.LLEP_MAX_FFN_DIM or not 0 < F <= B.LLEP_MAX_FFN_DIM:
+            raise ValueError("D and F must be multiples of 64, at most LLEP_MAX_FFN_DIM")
+        self.E, self.D, self.F = E, D, F
+        self.gate_up = B.llep_pack_matrix_mxfp4(w_gate, gate_scale, w_up, up_scale, D, stream)
+        self.down = B.llep_pack_matrix_mxfp4(w_down, down_scale, K=F, stream=stream)
+
+    @classmethod
+    def from_weights(cls, w_gate, w_up, w_down, stream=None):
+        """From the weights that llep_pack_weights takes: w_gate, w_up [E, D, F] and w_down
+        [E, F, D] in bf16 or float32."""
+        import torch
+        parts = []
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            for w in (w_gate, w_up, w_down):
+                E, K, N = w.shape
+                rows = w.transpose(1, 2).reshape(E * N, K)
+                for n in (B.llep_mxfp4_row_bytes(K), B.llep_mxfp4_scale_bytes(K)):
+                    parts.append(torch.empty((E * N, n), dtype=torch.uint8, device=w.device))
+                B.llep_quantize_rows_mxfp4(rows, *parts[-2:])
+                parts[-2:] = (t.view(E, N, -1) for t in parts[-2:])
+            return cls(*parts, D=w_gate.shape[1], F=w_gate.shape[2])
+
+
+class Router:
+    """Router logits to the ids and gates of a layer, and back (llep_route in llep.h).
+
+    score "softmax" or "sigmoid"; bias [E] float32 (of load balancing) or None, in the choice
+    alone; groups of experts of which the top_groups best are chosen from, by their best expert
+    ("max") or the sum of their two best ("top2"); gates renormalized over the chosen experts, times
+    scale. ids and gates are this object's buffers, the current stream's as in LLEPLayer.
+    """
+
+    def __init__(self, T: int, K: int, E: int, score: str = "softmax", bias=None, groups: int = 1,
+                 top_groups: int = 1, group_score: str = "max", renormalize: bool = True,
+                 scale: float = 1.0, device="cuda"):
+        import torch
+        self.params = B.make_route(T, K, E, score, groups, top_groups, group_score, renormalize,
+                                   scale)
+        self.bias = bias
+        self.ids = torch.empty((T, K), dtype=torch.int32, device=device)
+        self.gates = torch.empty((T, K), dtype=torch.float32, device=device)
+
+    def forward(self, logits, stream=None):
+        """(ids [T, K] int32, gates [T, K] float32) for logits [T, E] (bf16 or float32)."""
+        B.llep_route(self.params, logits, self.bias, self.ids, self.gates, stream)
+        return self.ids, self.gates
+
+    def backward(self, logits, d_gates, stream=None):
+        """d_logits [T, E] of the last forward(), whose logits these are, in their type."""
+        if getattr(self, "d_logits", None) is None or self.d_logits.dtype != logits.dtype:
+            self.d_logits = B._empty((self.params.T, self.params.E), logits.dtype, logits.device,
+                                     stream)
+        B.llep_route_backward(self.params, logits, self.ids, self.gates, d_gates, self.d_logits,
+                              stream)
+        return self.d_logits
+
+
 class LLEPLayer:
     """Buffers and calls for one layer shape.
 
@@ -202,6 +279,50 @@ class LLEPLayer:
         B.llep_permute(self.params, self.bufs, ids, gates, x.view(torch.bfloat16),
                        self.x_perm_q.view(torch.bfloat16), self.gate_perm, self.row_pair,
                        self.pair_row, stream)
+
+    def forward_mxfp4(self, ids, gates, x, experts: Mxfp4Experts, device: int = -1, stream=None):
+        """forward() for serving with 4-bit experts (bf16 layers): the tokens to 4-bit rows, then
+        plan -> permute (of those rows) -> grouped FFN in 4 bits -> combine. Returns y (valid for
+        every token only when device == -1). backward() is not available after it; a call that is
+        refused changes nothing."""
+        import torch
+        if self.dtype != torch.bfloat16:
+            raise TypeError("forward_mxfp4 needs a bf16 layer")
+        if (experts.E, experts.D, experts.F) != (self.E, self.D, self.F):
+            raise ValueError("the experts do not fit this layer")
+        if not -1 <= device < self.P:
+            raise ValueError("device outside [-1, P)")
+        self.check_routing(ids, gates)
+        B._dense("x", x, (self.T, self.D), x.dtype)
+        B._dtype_code(x)
+        B._here(ids, gates, x, self.y, experts.gate_up)
+        if not hasattr(self, "mxfp4_workspace"):
+            self._make_mxfp4_buffers(stream)
+        B.llep_quantize_rows_mxfp4(x, self.x_mx[:, :self.mx_values], self.x_mx[:, self.mx_values:],
+                                   stream)
+        self.gate_up_device = None
+        self.rows_are_int8 = True  # x_perm holds no rows of this call
+        self.plan(ids, stream)
+        B.llep_permute(self.params, self.bufs, ids, gates, self.x_mx.view(torch.bfloat16),
+                       self.x_perm_mx.view(torch.bfloat16), self.gate_perm, self.row_pair,
+                       self.pair_row, stream)
+        B.llep_grouped_ffn_mxfp4(self.params, self.bufs, device, self.x_perm_mx, experts.gate_up,
+                                 experts.down, self.D, self.F, self.out_perm_mx,
+                                 self.mxfp4_workspace, stream)
+        B.llep_combine_to_bf16(self.params, self.out_perm_mx, self.pair_row, gates, self.y, stream)
+        return self.y
+
+    def _make_mxfp4_buffers(self, stream):
+        import torch
+        R, D, dev = max(self.T * self.K, 1), self.D, self.device
+        self.mx_values = B.llep_mxfp4_row_bytes(D)
+        row = self.mx_values + B.llep_mxfp4_scale_bytes(D)
+        self.x_mx = B._empty((self.T, row), torch.uint8, dev, stream)
+        self.x_perm_mx = B._empty((R, row), torch.uint8, dev, stream)
+        # the experts' outputs stay in float32, so that y is rounded once
+        self.out_perm_mx = B._empty((R, D), torch.float32, dev, stream)
+        nbytes = B.llep_grouped_ffn_mxfp4_workspace_bytes(self.params, self.F)
+        self.mxfp4_workspace = B._empty((nbytes,), torch.uint8, dev, stream)
 
     def _saved_covers(self, device: int) -> bool:
         saved = getattr(self, "gate_up_device", None)
