@@ -47,3 +47,20 @@ from .llep import (  # noqa: F401
     standard_ep_assignment,
     swiglu_ffn,
 )
+from .route import (  # noqa: F401
+    choose,
+    gates_of,
+    route,
+    route_backward,
+    route_scores,
+)
+from .mxfp4 import (  # noqa: F401
+    mxfp4_codes,
+    mxfp4_decode,
+    mxfp4_doubt,
+    mxfp4_exponents,
+    mxfp4_pack,
+    mxfp4_round,
+    mxfp4_unpack,
+    swiglu_ffn_mxfp4,
+)

@@ -8,7 +8,7 @@ from __future__ import annotations
 from typing import Optional
 
 from . import binding as B
-from .layer import Int8Experts, LLEPLayer
+from .layer import Int8Experts, LLEPLayer, Mxfp4Experts
 
 
 class ExpertBlock:
@@ -55,6 +55,14 @@ class ExpertBlock:
         B.llep_block_norm(x, None, None, None, self.w_pre, self.alpha, self.eps, None, None,
                           self.h_q, self.h_scale, stream)
         y = self.layer.forward_int8(ids, gates, self.h_q, experts, -1, stream, self.h_scale)
+        return self._after(x, y, stream)
+
+    def forward_mxfp4(self, ids, gates, x, experts: Mxfp4Experts, stream=None):
+        """Serving forward with 4-bit experts (bf16 layers). Returns (r, h_next)."""
+        self.layer.check_mxfp4(ids, gates, self.h, experts)
+        B.llep_block_norm(x, None, None, None, self.w_pre, self.alpha, self.eps, None, self.h,
+                          stream=stream)
+        y = self.layer.forward_mxfp4(ids, gates, self.h, experts, -1, stream)
         return self._after(x, y, stream)
 
     def _after(self, x, y, stream):

@@ -349,6 +349,48 @@ struct LaunchSched {
   __device__ __forceinline__ void done(const TileCoord &, bool) {}
 };
 
+// Hand-out of a dense product's tiles: those of LaunchSched, computed from M.
+template <int BM, int BN>
+struct DenseSched {
+  static constexpr int kBM = BM;
+  static constexpr bool kAnyC = true;
+  static constexpr bool kOpaqueLane = false;
+  static constexpr bool kCoherentC = false;
+  int64_t M;
+  int N, nk, n_mt, n_nt, G, slot, it;
+  template <class Args>
+  __device__ __forceinline__ explicit DenseSched(const Args &g) {
+    M = g.M;
+    N = g.N;
+    nk = g.Kdim / kSK;
+    n_mt = int((M + BM - 1) / BM);
+    n_nt = (N + BN - 1) / BN;
+    G = gridDim.x;
+    slot = (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8;
+    it = 0;
+  }
+  __device__ __forceinline__ bool tile(int64_t u, TileCoord &t) const {
+    if (u >= int64_t(n_mt) * n_nt) return false;
+    const int sr = int(u / (int64_t(kGroupM) * n_nt));
+    const int rem = int(u - int64_t(sr) * kGroupM * n_nt);
+    const int gm = min(kGroupM, n_mt - sr * kGroupM);
+    t.e = 0;
+    t.row0 = 0;
+    t.prow0 = 0;
+    t.mt = sr * kGroupM + rem % gm;
+    t.m0 = t.mt * BM;
+    t.rows_valid = int(min<int64_t>(BM, M - t.m0));
+    t.n0 = rem / gm * BN;
+    t.cols_valid = min(BN, N - t.n0);
+    t.nk = nk;
+    return true;
+  }
+  __device__ __forceinline__ bool first(TileCoord &t) const { return tile(slot, t); }
+  __device__ __forceinline__ void request() {}
+  __device__ __forceinline__ bool next(TileCoord &t) { return tile(int64_t(++it) * G + slot, t); }
+  __device__ __forceinline__ void done(const TileCoord &, bool) {}
+};
+
 // A is row-major (lda) or, with kABlocked, in 16 x 32 blocks over padded
 // rows; C likewise with kCBlocked. B is always in 16 x 32 blocks.
 //

@@ -13,12 +13,10 @@
 #include <algorithm>
 #include <cmath>
 
-#include "gemm.h"
+#include "mx_tiles.h"
 #include "rows.h"
 
 namespace llep {
-
-typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSliceK = 128;     // values of a row in a slice
 constexpr int kBlockK = 32;      // that share an exponent
@@ -28,31 +26,6 @@ static int32_t mx_row_bytes(int32_t K) { return mx_slices(K) * 64; }
 static int32_t mx_scale_bytes(int32_t K) { return (mx_slices(K) + kScaleSlices - 1) / kScaleSlices * 16; }
 int32_t mxfp4_row_bytes(int32_t K) { return mx_row_bytes(K); }
 int32_t mxfp4_scale_bytes(int32_t K) { return mx_scale_bytes(K); }
-
-// ---------------------------------------------------------------------------
-// 4-bit values: sign, two bits of exponent, one of fraction (0, 0.5, 1, 1.5, 2,
-// 3, 4, 6). The exponent of a block whose largest magnitude has the (biased)
-// exponent field e is e - 2 (4 = 2^2 is the largest power of two among the
-// values), at least 1; a block with an infinity or a NaN gets 255, which makes
-// all of it NaN. Values are rounded to the nearest, ties to the even one, and
-// are at most 6.
-// ---------------------------------------------------------------------------
-
-__device__ __forceinline__ uint32_t mx_exponent(uint32_t most_bits) {
-  const uint32_t e = most_bits >> 23;
-  return e == 255u ? 255u : uint32_t(max(int(e) - 2, 1));
-}
-// the power of two (of 255: any number, the values do not matter)
-__device__ __forceinline__ float mx_step(uint32_t exponent) {
-  return __uint_as_float(min(exponent, 254u) << 23);
-}
-// four values in 16 bits
-__device__ __forceinline__ uint32_t mx_pack4(float a, float b, float c, float d, float step) {
-  uint32_t v = 0;
-  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, a, b, step, 0);
-  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, c, d, step, 1);
-  return v;
-}
 
 // ---------------------------------------------------------------------------
 // rows: a wavefront per 512 values of a row, 8 per lane, so that a block's
@@ -271,42 +244,6 @@ hipError_t launch_pack_mxfp4(int32_t E, int32_t N, int32_t K, const uint8_t *w0,
 // products
 // ---------------------------------------------------------------------------
 
-// A: rows of lda bytes (64 a slice) with their exponents lds_a bytes apart; of
-// the base, A, lda, B and b_expert_stride count bytes here, Kdim 32 a slice.
-struct MxGemmArgs : GemmArgs {
-  const uint8_t *a_scale;
-  int64_t a_scale_pitch;
-  int64_t b_scale_at;          // of an expert's exponents behind its values, bytes
-  int64_t b_scale_blk_stride;  // bytes per 16-row block across all of K
-  int64_t M;                   // dense: rows of A
-  bool f32_out;
-  // SwiGLU: rows of ldc bytes with the exponents of the activation
-  uint8_t *act, *act_scale;
-  int32_t act_blocks;          // exponents of a row that a product reads
-};
-
-__device__ __forceinline__ i32x8 mx_operand(const i32x4 v) {
-  return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
-}
-// the exponents are bytes kSel of the two scale operands
-template <int kSel>
-__device__ __forceinline__ f32x4 mx_mfma(const i32x4 b, const i32x4 a, const f32x4 c, int sb, int sa) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(b), mx_operand(a), c, 4, 4,
-                                                          kSel, sb, kSel, sa);
-}
-template <int kSel>
-__device__ __forceinline__ f32x16 mx_mfma(const i32x4 b, const i32x4 a, const f32x16 c, int sb, int sa) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(b), mx_operand(a), c, 4, 4,
-                                                         kSel, sb, kSel, sa);
-}
-__device__ __forceinline__ float mx_swiglu(float g, float u) {
-  return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
-}
-// the exponents behind a row's last block, up to those that a product reads
-__device__ __forceinline__ void mx_pad_scales(uint8_t *row, int blocks, int read) {
-  for (int b = blocks; b < read; ++b) row[b] = 127;
-}
-
 // Stream: few rows. An item is up to 16 kMB rows of one group (of A, dense) by
 // 16 kNB packed rows of the weights; a workgroup of kWaves wavefronts takes one
 // item at a time, each wavefront a part of k, and adds the parts up through
@@ -320,6 +257,7 @@ template <int kMB, int kNB, int kWaves, bool kGrouped, bool kSwigluOut>
 __global__ __launch_bounds__(kWaves * kWave) void mx_stream_kernel(MxGemmArgs g) {
   constexpr int kBlocks = kMB * kNB;
   constexpr int kRound = kBlocks >= 16 ? 8 : kBlocks;
+  constexpr int kUnroll = kMB * kNB <= 8 ? 4 : 2;  // slices
   __shared__ f32x4 part[kWaves][kRound][kWave];
   static_assert(!kSwigluOut || kNB == 4, "32 gate columns and the matching up columns");
   static_assert(kBlocks % kRound == 0 && kRound % kNB == 0, "rounds of whole rows of blocks");
@@ -373,27 +311,47 @@ __global__ __launch_bounds__(kWaves * kWave) void mx_stream_kernel(MxGemmArgs g)
     for (int m = 0; m < kMB; ++m)
 #pragma unroll
       for (int n = 0; n < kNB; ++n) acc[m][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int kb = kb0; kb < kb1; ++kb) {
-      i32x4 fa[kMB], fb[kNB];
-      int sa[kMB], sb[kNB];
+    // kU slices at a time, all of their loads under way together
+    auto steps = [&](auto count, int kb) {
+      constexpr int kU = decltype(count)::value;
+      i32x4 fa[kU][kMB], fb[kU][kNB];
+      int sa[kU][kMB], sb[kU][kNB];
 #pragma unroll
-      for (int n = 0; n < kNB; ++n) {
-        fb[n] = *reinterpret_cast<const i32x4 *>(B + int64_t(kb) * 1024 + offB[n]);
-        sb[n] = *reinterpret_cast<const int32_t *>(Bs + (kb >> 2) * 256 + (kb & 3) * 4 + offBs[n]);
+      for (int u = 0; u < kU; ++u) {
+        const int k = kb + u;
+#pragma unroll
+        for (int n = 0; n < kNB; ++n) {
+          fb[u][n] = *reinterpret_cast<const i32x4 *>(B + int64_t(k) * 1024 + offB[n]);
+          sb[u][n] = *reinterpret_cast<const int32_t *>(Bs + (k >> 2) * 256 + (k & 3) * 4 + offBs[n]);
+        }
+#pragma unroll
+        for (int m = 0; m < kMB; ++m) {
+          fa[u][m] = *reinterpret_cast<const i32x4 *>(A + k * 64 + offA[m]);
+          sa[u][m] = *reinterpret_cast<const int32_t *>(As + k * 4 + offAs[m]);
+        }
       }
+      // (the lane's 32 values have byte lane / 16 of the four)
 #pragma unroll
-      for (int m = 0; m < kMB; ++m) {
-        fa[m] = *reinterpret_cast<const i32x4 *>(A + kb * 64 + offA[m]);
-        sa[m] = *reinterpret_cast<const int32_t *>(As + kb * 4 + offAs[m]);
+      for (int u = 0; u < kU; ++u) {
+#pragma unroll
+        for (int n = 0; n < kNB; ++n) sb[u][n] = int(uint32_t(sb[u][n]) >> shift);
+#pragma unroll
+        for (int m = 0; m < kMB; ++m) {
+          sa[u][m] = int(uint32_t(sa[u][m]) >> shift);
+#pragma unroll
+          for (int n = 0; n < kNB; ++n)
+            acc[m][n] = mx_mfma<0>(fb[u][n], fa[u][m], acc[m][n], sb[u][n], sa[u][m]);
+        }
       }
-#pragma unroll
-      for (int n = 0; n < kNB; ++n) sb[n] = int(uint32_t(sb[n]) >> shift);
-#pragma unroll
-      for (int m = 0; m < kMB; ++m) {
-        sa[m] = int(uint32_t(sa[m]) >> shift);
-#pragma unroll
-        for (int n = 0; n < kNB; ++n) acc[m][n] = mx_mfma<0>(fb[n], fa[m], acc[m][n], sb[n], sa[m]);
-      }
+    };
+    int kb = kb0;
+    for (; kb + kUnroll <= kb1; kb += kUnroll) steps(std::integral_constant<int, kUnroll>{}, kb);
+    // the rest together: one wait, not one for each
+    switch (kb1 - kb) {
+      case 3: steps(std::integral_constant<int, 3>{}, kb); break;
+      case 2: steps(std::integral_constant<int, 2>{}, kb); break;
+      case 1: steps(std::integral_constant<int, 1>{}, kb); break;
+      default: break;
     }
 #pragma unroll
     for (int b0 = 0; b0 < kBlocks; b0 += kRound) {
@@ -462,7 +420,37 @@ hipError_t run_mx_stream(const MxGemmArgs &g, int64_t mtiles, hipStream_t stream
   return hipGetLastError();
 }
 
-static MxGemmArgs mx_weights(const uint8_t *w, int32_t N, int32_t K, bool swiglu) {
+// BM x BM tiles: 256 rows by eight wavefronts, one workgroup on a compute unit,
+// or 128 by four, two workgroups; two wavefronts per SIMD either way.
+template <int BM, int WAVES_M, int WAVES_N, int kEpi, bool kGrouped>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void mx_tiles_kernel(MxGemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char smem[mx_ring_bytes<BM, BM>()];
+  std::conditional_t<kGrouped, LaunchSched<BM, BM>, DenseSched<BM, BM>> sched(g);
+  TileCoord t;
+  if (!sched.first(t)) return;
+  mx_tiles<BM, WAVES_M, WAVES_N, kEpi>(g, smem, t, sched);
+}
+
+template <int BM, int kEpi, bool kGrouped>
+hipError_t run_mx_tiles(const MxGemmArgs &g, hipStream_t stream) {
+  constexpr int WAVES_M = 2, WAVES_N = BM / 64;
+  int64_t most = cu_count() * (BM == 256 ? 1 : 2);
+  if (!kGrouped) most = std::min(most, (g.M + BM - 1) / BM * ((g.N + BM - 1) / BM));
+  const int grid = int((most + 7) / 8 * 8);
+  hipLaunchKernelGGL((mx_tiles_kernel<BM, WAVES_M, WAVES_N, kEpi, kGrouped>), dim3(grid),
+                     dim3(64 * WAVES_M * WAVES_N), 0, stream, g);
+  return hipGetLastError();
+}
+
+// outputs in bfloat16 or float32
+template <int BM, bool kGrouped>
+hipError_t run_mx_tiles_out(const MxGemmArgs &g, hipStream_t stream) {
+  return g.f32_out ? run_mx_tiles<BM, kMxF32, kGrouped>(g, stream)
+                   : run_mx_tiles<BM, kMxBf16, kGrouped>(g, stream);
+}
+
+static MxGemmArgs mx_weights(const uint8_t *w, int32_t N, int32_t K) {
   MxGemmArgs g = {};
   g.B = reinterpret_cast<const uint16_t *>(w);
   g.b_expert_stride = int64_t(packed_mxfp4_bytes(N, K));
@@ -471,13 +459,12 @@ static MxGemmArgs mx_weights(const uint8_t *w, int32_t N, int32_t K, bool swiglu
   g.b_scale_blk_stride = int64_t(mx_scale_bytes(K)) * 16;
   g.N = N;
   g.Kdim = mx_slices(K) * 32;
-  (void)swiglu;
   return g;
 }
 
 hipError_t launch_mxfp4_matmul(const MxMatmulArgs &a, hipStream_t stream) {
   if (a.M == 0) return hipSuccess;
-  MxGemmArgs g = mx_weights(a.w, a.N, a.K, false);
+  MxGemmArgs g = mx_weights(a.w, a.N, a.K);
   g.A = reinterpret_cast<const uint16_t *>(a.x);
   g.lda = a.x_pitch;
   g.a_scale = a.x_scale;
@@ -486,8 +473,40 @@ hipError_t launch_mxfp4_matmul(const MxMatmulArgs &a, hipStream_t stream) {
   g.ldc = a.N;
   g.M = a.M;
   g.f32_out = a.dtype == LLEP_F32;
-  if (a.M <= 16) return run_mx_stream<1, 4, 4, false, false>(g, 1, stream);
-  return run_mx_stream<4, 4, 4, false, false>(g, (a.M + 63) / 64, stream);
+  // The least of what the ways take in us, about: the stream with 32 or 64 rows
+  // and columns an item, by rounds of 256 items, the tiles by rounds of as many as
+  // the chip has room for (of 128 x 128 two on a compute unit).
+  // Stream of 32 / of 64 / tiles of 128 / of 256, M x N x K:
+  //   32 x 2880 x 2880 5.6 / 7.8 / 12.6 / -, 64 x 7168 x 2048 7.7 / 8.8 / 10.5 / 13.6,
+  //   128 x 2048 x 7168 11.2 / 20.6 / 27.7 / 37, 256 x 4096 x 4096 22.8 / 13.8 / 17.8 / -,
+  //   256 x 7168 x 2048 23.4 / 16.7 / 11.2 / 16.7, 512 x 2048 x 7168 36 / 21 / 28 / 42,
+  //   512 x 4096 x 4096 42 / 26 / 18 / -, 1024 x 7168 x 2048 64 / 53 / 14.8 / 17.8,
+  //   2000 x 4096 x 768 34 / 35 / 9.6 / 11.6, 4096 x 2880 x 2880 - / 108 / 38 / 26,
+  //   8192 x 7168 x 2048 - / - / 96 / 83, 8192^3 - / - / 356 / 262
+  const double k = a.K;
+  auto items = [&](int64_t n) { return double((a.M + n - 1) / n) * double((a.N + n - 1) / n); };
+  const double stream32 =
+      2.3 + 1.25e-3 * k + std::max(0.0, items(32) / 256 - 1) * (0.8 + 1.05e-3 * k);
+  const double stream64 = (4.5 + 2.2e-3 * k) * std::ceil(items(64) / 256);
+  const double cus = cu_count();
+  const double ring128 = items(128) <= cus ? 4.5 + 3.2e-3 * k
+                                           : (3 + 5.1e-3 * k) * std::ceil(items(128) / (2 * cus));
+  const double ring256 = items(256) <= cus / 2 ? 5.5 + 5.2e-3 * k
+                                               : (6 + 7.3e-3 * k) * std::ceil(items(256) / cus);
+  const double best = std::min(std::min(stream32, stream64), std::min(ring128, ring256));
+  // up to 16 rows: units of 16 columns, more of which are at work (1 row, 16 / 32 / 64
+  // columns: 7168 x 2048 3.8 / 3.5 / 4.2, 768 x 7168 4.1 / 5.4 / 7.7, 16384^2 22 / 25 / 27)
+  if (a.M <= 16) return run_mx_stream<1, 1, 8, false, false>(g, 1, stream);
+  if (best == stream32) {
+    // few items: more wavefronts for k (32 x 2048 x 7168 11.1 -> 7.3, 64 rows 11.0 -> 7.5,
+    // but 64 x 4096 x 4096 7.8 -> 10.8)
+    const int64_t mt = (a.M + 31) / 32;
+    if (mt * ((a.N + 15) / 16) <= 256) return run_mx_stream<2, 1, 16, false, false>(g, mt, stream);
+    return run_mx_stream<2, 2, 8, false, false>(g, mt, stream);
+  }
+  if (best == stream64) return run_mx_stream<4, 4, 8, false, false>(g, (a.M + 63) / 64, stream);
+  return best == ring128 ? run_mx_tiles_out<128, false>(g, stream)
+                         : run_mx_tiles_out<256, false>(g, stream);
 }
 
 // Workspace of the grouped FFN: the tile count (int at 0), the tile list, and
@@ -509,6 +528,27 @@ size_t ffn_mxfp4_workspace_bytes(int64_t R, int32_t E, int32_t P, int32_t F) {
   return mx_ws(R, E, P, F).total;
 }
 
+// Rows of a tile, by the rows per expert on average (the routing is not known
+// here): the stream's 16, or tiles of 128 or 256. Whole layers in us, uniform
+// routing unless "hot" (60% of the pairs on four experts):
+//   2880 x 2880, 32 experts, 4 of them a token, 16 / 128 / 256 rows:
+//     8 tokens 68 / 72 / -, 64 hot 121 / 125 / -, 128 135 / 115 / 120,
+//     and 128 / 256: 250 tokens 128 / 125, 400 hot 159 / 153, 1000 204 / 173,
+//     8192 hot 902 / 688
+//   2048 x 768, 128 experts, 8: 16 tokens 55 / 64 / -, 128 96 / 93 / -,
+//     700 - / 121 / 122, 1531 - / 158 / 148, 2200 hot - / 200 / 201, 4096 - / 316 / 282
+//   1024 x 768, 16 experts, 2: 100 tokens 30 / 38 / -, 300 36 / 40 / 41,
+//     700 47 / 43 / 45, 2000 - / 50 / 59
+// (With 32 or 64 rows the stream is slower than the better of these in all of them
+// but 300 tokens of the last, 35.)
+static int ffn_mxfp4_rows(const FfnMxArgs &a) {
+  const int64_t R = a.R, E = a.E, weight = int64_t(a.D) * a.F;
+  if (R <= 8 * E || weight * R <= int64_t(500000000)) return 16;
+  // 256 rows where many would be valid, and a few rounds of such tiles
+  const int64_t tiles = (R / 256 + E) * ((a.F + 127) / 128);
+  return R > 30 * E && tiles >= 512 ? 256 : 128;
+}
+
 hipError_t launch_ffn_mxfp4(const FfnMxArgs &a, hipStream_t stream) {
   if (a.R == 0) return hipSuccess;
   const MxWs w = mx_ws(a.R, a.E, a.P, a.F);
@@ -516,12 +556,12 @@ hipError_t launch_ffn_mxfp4(const FfnMxArgs &a, hipStream_t stream) {
   int32_t *n_mtiles = reinterpret_cast<int32_t *>(ws);
   int4 *tiles = reinterpret_cast<int4 *>(ws + w.tiles);
   uint8_t *act = reinterpret_cast<uint8_t *>(ws + w.act);
-  const int rows = a.R <= 8 * int64_t(a.E) ? 16 : 64;
+  const int rows = ffn_mxfp4_rows(a);
   hipError_t err = launch_tile_table(a.groups, a.group_begin, 2 * a.E + a.P, a.device, a.P, rows,
                                      tiles, n_mtiles, stream);
   if (err != hipSuccess) return err;
   const int64_t mt_most = a.R / rows + std::min<int64_t>(a.R, 2 * int64_t(a.E) + a.P);
-  MxGemmArgs g = mx_weights(a.w_gate_up, 2 * a.F, a.D, true);
+  MxGemmArgs g = mx_weights(a.w_gate_up, 2 * a.F, a.D);
   g.A = reinterpret_cast<const uint16_t *>(a.x_perm);
   g.lda = g.a_scale_pitch = mx_pair_bytes(a.D);
   g.a_scale = a.x_perm + mx_row_bytes(a.D);
@@ -532,10 +572,11 @@ hipError_t launch_ffn_mxfp4(const FfnMxArgs &a, hipStream_t stream) {
   g.act_scale = act + mx_row_bytes(a.F);
   g.act_blocks = mx_slices(a.F) * 4;
   g.ldc = mx_pair_bytes(a.F);
-  err = rows == 16 ? run_mx_stream<1, 4, 4, true, true>(g, mt_most, stream)
-                   : run_mx_stream<4, 4, 4, true, true>(g, mt_most, stream);
+  err = rows == 16    ? run_mx_stream<1, 4, 4, true, true>(g, mt_most, stream)
+        : rows == 128 ? run_mx_tiles<128, kMxSwiglu, true>(g, stream)
+                      : run_mx_tiles<256, kMxSwiglu, true>(g, stream);
   if (err != hipSuccess) return err;
-  MxGemmArgs d = mx_weights(a.w_down, a.D, a.F, false);
+  MxGemmArgs d = mx_weights(a.w_down, a.D, a.F);
   d.A = reinterpret_cast<const uint16_t *>(act);
   d.lda = d.a_scale_pitch = mx_pair_bytes(a.F);
   d.a_scale = act + mx_row_bytes(a.F);
@@ -545,8 +586,9 @@ hipError_t launch_ffn_mxfp4(const FfnMxArgs &a, hipStream_t stream) {
   d.C = static_cast<uint16_t *>(a.out_perm);
   d.ldc = a.D;
   d.f32_out = a.f32_out;
-  return rows == 16 ? run_mx_stream<1, 4, 4, true, false>(d, mt_most, stream)
-                    : run_mx_stream<4, 4, 4, true, false>(d, mt_most, stream);
+  return rows == 16    ? run_mx_stream<1, 4, 4, true, false>(d, mt_most, stream)
+         : rows == 128 ? run_mx_tiles_out<128, true>(d, stream)
+                       : run_mx_tiles_out<256, true>(d, stream);
 }
 
 }  // namespace llep

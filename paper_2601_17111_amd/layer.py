@@ -280,11 +280,8 @@ class LLEPLayer:
                        self.x_perm_q.view(torch.bfloat16), self.gate_perm, self.row_pair,
                        self.pair_row, stream)
 
-    def forward_mxfp4(self, ids, gates, x, experts: Mxfp4Experts, device: int = -1, stream=None):
-        """forward() for serving with 4-bit experts (bf16 layers): the tokens to 4-bit rows, then
-        plan -> permute (of those rows) -> grouped FFN in 4 bits -> combine. Returns y (valid for
-        every token only when device == -1). backward() is not available after it; a call that is
-        refused changes nothing."""
+    def check_mxfp4(self, ids, gates, x, experts: Mxfp4Experts, device: int = -1):
+        """Refuses what forward_mxfp4() does not take."""
         import torch
         if self.dtype != torch.bfloat16:
             raise TypeError("forward_mxfp4 needs a bf16 layer")
@@ -296,6 +293,14 @@ class LLEPLayer:
         B._dense("x", x, (self.T, self.D), x.dtype)
         B._dtype_code(x)
         B._here(ids, gates, x, self.y, experts.gate_up)
+
+    def forward_mxfp4(self, ids, gates, x, experts: Mxfp4Experts, device: int = -1, stream=None):
+        """forward() for serving with 4-bit experts (bf16 layers): the tokens to 4-bit rows, then
+        plan -> permute (of those rows) -> grouped FFN in 4 bits -> combine. Returns y (valid for
+        every token only when device == -1). backward() is not available after it; a call that is
+        refused changes nothing."""
+        import torch
+        self.check_mxfp4(ids, gates, x, experts, device)
         if not hasattr(self, "mxfp4_workspace"):
             self._make_mxfp4_buffers(stream)
         B.llep_quantize_rows_mxfp4(x, self.x_mx[:, :self.mx_values], self.x_mx[:, self.mx_values:],
@@ -329,9 +334,9 @@ class LLEPLayer:
         return saved is not None and (saved == -1 or saved == device)
 
     def check_backward(self):
-        """Refuses a backward() whose rows forward_int8() has replaced."""
+        """Refuses a backward() whose rows forward_int8() or forward_mxfp4() has replaced."""
         if getattr(self, "rows_are_int8", False):
-            raise RuntimeError("backward() after forward_int8()")
+            raise RuntimeError("backward() after forward_int8() or forward_mxfp4()")
 
     def backward(self, dy, gates, w_gate_up, w_gate_up_t, w_down_t, device: int = -1,
                  stream=None):
