@@ -1,0 +1,378 @@
+"""Routing and its gradient against the oracle: ids exactly, over numbers of
+experts from one to the largest, odd ones, every form of score and group, masked
+experts and rows, ties, and keys that float32 does not tell apart; refusals of
+the binding are in test_route_host.py.
+
+Tolerances, in units u = 2^-24 of a result's size. A gate is e^z over a sum: the
+difference z is rounded once (at most |z| u; logits here lie within 16 of each
+other, log-sigmoids take three roundings more), the exponential and the
+quotient take 2 each, the sum of at most 512 terms in at most 40 steps 40, the
+factor 1: 64 in all are allowed. Below 2^-126 float32's steps stay 2^-149, so that
+there the exponential's step, half of one of the quotient, both times the factor,
+and half of one of the product count: 2^-149 (1.5 scale + 0.5) more, whatever the
+gate's size (1 and 6 10^-44: a relative bound alone is below half of such a step).
+A gradient is a sum of at most K + 1 products
+of a gate (64), a difference of two numbers (each within 64 + K of the largest
+|d gate|) and a slope (4): (200 + 2 K) u of scale max|d gate| max gate, and half a
+step of a bfloat16 result. The gradient reads the gates that the forward left, so
+these are rounded before it."""
+
+import math
+
+import numpy as np
+import pytest
+
+import oracle
+from gpu_util import device
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+INF = math.inf
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return device()
+
+
+def _route(dev, logits, K, bias=None, dtype=None, **how):
+    import torch
+    from paper_2601_17111_amd import binding as B
+    T, E = logits.shape
+    x = logits.to(dev) if dtype is None else logits.to(dtype).to(dev)
+    p = B.make_route(T, K, E, **how)
+    ids = torch.full((T, K), 77, dtype=torch.int32, device=dev)
+    gates = torch.full((T, K), -7.0, device=dev)
+    b = None if bias is None else bias.float().to(dev)
+    B.llep_route(p, x, b, ids, gates)
+    torch.cuda.synchronize()
+    return p, x, b, ids, gates
+
+
+def _check(dev, logits, K, bias=None, dtype=None, **how):
+    p, x, b, ids, gates = _route(dev, logits, K, bias, dtype, **how)
+    want_ids, want = oracle.route(x.float().cpu().numpy(), K,
+                                  bias=None if b is None else b.cpu().numpy(), **how)
+    assert np.array_equal(ids.cpu().numpy(), want_ids)
+    got = gates.double().cpu().numpy()
+    near = 64 * U * np.abs(want) + 2.0 ** -149 * (1.5 * how.get("scale", 1.0) + 0.5)
+    assert np.all(np.abs(got - want) <= near), np.abs(got - want).max()
+    return p, x, ids, gates
+
+
+def _logits(seed, T, E, masked=0.0, spread=1.5):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    l = (torch.randn(T, E, generator=g) * spread).clamp(-8, 8)
+    if masked:
+        l[torch.rand(T, E, generator=g) < masked] = -INF
+        l[torch.rand(T, generator=g) < masked] = -INF
+    return l, torch.randn(E, generator=g) * 0.1
+
+
+SHAPES = [(1, 1, 1), (1, 256, 8), (3, 5, 5), (7, 37, 2), (130, 32, 4), (67, 128, 8), (33, 160, 6),
+          (20, 512, 8), (5, 511, 3), (9, 64, 16), (6, 96, 64), (4, 512, 64), (11, 100, 9)]
+
+
+@pytest.mark.parametrize("T,E,K", SHAPES)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_forms(dev, T, E, K, score, bias, dtype):
+    import torch
+    l, b = _logits(T * 1000 + E, T, E)
+    _check(dev, l, K, b if bias else None, getattr(torch, dtype), score=score,
+           renormalize=(E + K) % 2 == 0, scale=2.5)
+
+
+@pytest.mark.parametrize("E,G,top,K", [(256, 8, 4, 8), (256, 8, 3, 4), (64, 4, 2, 6), (160, 5, 2, 8),
+                                       (96, 12, 5, 7), (512, 64, 8, 8), (36, 6, 2, 5), (512, 2, 1, 8),
+                                       (128, 8, 1, 12), (24, 24, 5, 5), (64, 32, 20, 20),
+                                       (256, 4, 4, 8)])
+@pytest.mark.parametrize("by", ["max", "top2"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_groups(dev, E, G, top, K, by, bias):
+    l, b = _logits(E + G, 45, E, masked=0.1)
+    _check(dev, l, K, b if bias else None, score="sigmoid" if by == "top2" else "softmax", groups=G,
+           top_groups=top, group_score=by)
+
+
+@pytest.mark.parametrize("T,E,K", [(20000, 128, 8), (20000, 40, 4), (17000, 64, 5), (5000, 256, 8),
+                                   (4500, 33, 12)])
+def test_long_batches(dev, T, E, K):
+    """The kernels for many rows, on their last rows and a sample of the others."""
+    import torch
+    l, b = _logits(T, T, E, masked=0.05)
+    for dtype in (torch.float32, torch.bfloat16):
+        for bias in (None, b):
+            p, x, bd, ids, gates = _route(dev, l, K, bias, dtype)
+            at = np.concatenate([np.arange(200), np.arange(300, T, 97), np.arange(T - 70, T)])
+            rows = x.float().cpu().numpy()[at]
+            want_ids, want = oracle.route(rows, K, bias=None if bias is None else bias.numpy())
+            assert np.array_equal(ids.cpu().numpy()[at], want_ids)
+            got = gates.double().cpu().numpy()[at]
+            assert np.all(np.abs(got - want) <= 64 * U * np.abs(want))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("masked", [0.3, 0.95, 1.0])
+def test_masked_experts_and_rows(dev, score, renormalize, masked):
+    l, b = _logits(5, 60, 48, masked=masked)
+    for bias in (None, b):
+        for K in (8, 20):
+            _check(dev, l, K, bias, score=score, renormalize=renormalize)
+    b[::3] = -INF
+    _check(dev, l, 8, b, score=score, renormalize=renormalize, groups=4, top_groups=3,
+           group_score="top2")
+
+
+def test_lowest_values_are_not_masks(dev):
+    """The type's lowest finite value may be taken, an infinity below it not."""
+    import torch
+    low = torch.finfo(torch.float32).min
+    l = torch.tensor([[low, -INF, low, 0.0], [low, low, -INF, -INF], [-INF, -INF, -INF, low]])
+    for score in ("softmax", "sigmoid"):
+        _, _, _, ids, gates = _route(dev, l, 3, score=score)
+        assert ids.tolist() == [[3, 0, 2], [0, 1, -1], [3, -1, -1]]
+        g = gates.tolist()
+        assert g[0] == [1.0, 0.0, 0.0] and g[1] == [0.5, 0.5, 0.0] and g[2] == [1.0, 0.0, 0.0]
+
+
+def test_nan_and_infinity(dev):
+    import torch
+    nan = math.nan
+    l = torch.tensor([[nan, 1.0, 2.0, -1.0], [0.0, INF, 1.0, 2.0], [nan, nan, nan, nan]])
+    _, _, _, ids, gates = _route(dev, l, 2, score="sigmoid", renormalize=False)
+    assert ids.tolist() == [[2, 1], [1, 3], [-1, -1]]
+    assert gates[1, 0] == 1.0 and gates[2].tolist() == [0.0, 0.0]
+    # over all experts one NaN is everybody's
+    _, _, _, ids, gates = _route(dev, l[:1], 2, renormalize=False)
+    assert ids.tolist() == [[2, 1]] and bool(torch.isnan(gates).all())
+    # and its key with a bias is NaN: nothing is chosen
+    _, _, _, ids, gates = _route(dev, l[:1], 2, bias=torch.zeros(4), renormalize=False)
+    assert ids.tolist() == [[-1, -1]] and gates.tolist() == [[0.0, 0.0]]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("K", [4, 8, 10])
+def test_ties(dev, dtype, K):
+    """Few different logits, and biases: equal keys go to the lower index."""
+    import torch
+    g = torch.Generator().manual_seed(2)
+    l = torch.randint(-2, 3, (50, 64), generator=g).float()
+    b = torch.randint(0, 2, (64,), generator=g).float() * 0.25
+    for score in ("softmax", "sigmoid"):
+        _check(dev, l, K, None, getattr(torch, dtype), score=score)
+        _check(dev, l, K, b, getattr(torch, dtype), score=score)
+        _check(dev, l, K, b, getattr(torch, dtype), score=score, groups=4, top_groups=2,
+               group_score="top2")
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,G", [(32, 1), (200, 1), (256, 8)])
+def test_keys_that_float32_does_not_tell_apart(dev, score, E, G):
+    """Logits one step apart, under a large bias: the choice is that of float64 keys."""
+    import torch
+    g = torch.Generator().manual_seed(E)
+    l = torch.full((40, E), 0.75)
+    l += torch.randint(0, 64, l.shape, generator=g) * 2.0 ** -24
+    how = dict(groups=G, top_groups=G // 2, group_score="top2") if G > 1 else {}
+    _check(dev, l, 8, torch.full((E,), 3.0), score=score, **how)
+
+
+def test_large_logits(dev):
+    """Sigmoids that are 1 in float64 tie; logits without a bias do not."""
+    import torch
+    l = torch.tensor([[50.0, 60.0, 70.0, 80.0]])
+    _check(dev, l, 2, score="sigmoid")
+    _check(dev, l, 2, torch.zeros(4), score="sigmoid")
+    _check(dev, l * -10, 2, score="sigmoid")
+    _check(dev, l * 1000, 2, score="softmax")
+
+
+def test_unaligned_rows_and_neighbours(dev):
+    """Logits that start at any element; nothing beyond the outputs is written."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    T, E, K = 19, 37, 5
+    l, _ = _logits(1, T, E)
+    for dtype, off in ((torch.bfloat16, 1), (torch.bfloat16, 3), (torch.float32, 1)):
+        flat = torch.zeros(T * E + 8, dtype=dtype, device=dev)
+        x = flat[off:off + T * E].view(T, E)
+        x.copy_(l)
+        ids = torch.full((T * K + 8,), 77, dtype=torch.int32, device=dev)
+        gates = torch.full((T * K + 8,), -7.0, device=dev)
+        B.llep_route(B.make_route(T, K, E), x, None, ids[3:3 + T * K].view(T, K),
+                     gates[3:3 + T * K].view(T, K))
+        want_ids, want = oracle.route(x.float().cpu().numpy(), K)
+        assert np.array_equal(ids[3:3 + T * K].view(T, K).cpu().numpy(), want_ids)
+        for t, v in ((ids, 77), (gates, -7.0)):
+            assert t[:3].tolist() == [v] * 3 and t[3 + T * K:].tolist() == [v] * 5
+
+
+# ---------------------------------------------------------------------------
+# backward
+# ---------------------------------------------------------------------------
+
+def _check_backward(dev, logits, ids, K, dtype, score, renormalize, scale, d=None):
+    import torch
+    from paper_2601_17111_amd import binding as B
+    T, E = logits.shape
+    x = logits.to(dtype).to(dev)
+    rows = x.float().cpu().numpy()
+    g64 = np.array([oracle.gates_of(r, [int(e) if 0 <= e < E else -1 for e in i], score,
+                                    renormalize, scale) for r, i in zip(rows, ids.tolist())])
+    gates = torch.from_numpy(g64.reshape(T, K)).float().to(dev)
+    if d is None:
+        d = torch.randn(T, K, generator=torch.Generator().manual_seed(9)) * 0.1
+    dl = torch.full((T, E), 55.0, dtype=dtype, device=dev)
+    p = B.make_route(T, K, E, score=score, renormalize=renormalize, scale=scale)
+    reads = score == "sigmoid" or not renormalize
+    B.llep_route_backward(p, x if reads else None, ids.to(dev), gates, d.to(dev), dl)
+    torch.cuda.synchronize()
+    want = oracle.route_backward(rows, ids.tolist(), d.tolist(), score, renormalize, scale)
+    got = dl.double().cpu().numpy()
+    near = (200 + 2 * K) * U * float(d.abs().max()) * max(1.0, scale) * (1 + K)
+    if dtype == torch.bfloat16:
+        near = near + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(got - want) <= near), np.abs(got - want).max()
+    return x, gates, d, dl
+
+
+@pytest.mark.parametrize("T,E,K", [(1, 1, 1), (1, 256, 8), (9, 37, 2), (70, 128, 8), (5, 512, 64),
+                                   (4200, 40, 4), (4100, 300, 16)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_backward(dev, T, E, K, score, renormalize, dtype):
+    import torch
+    if T > 1000 and dtype == "bfloat16":
+        T, E = T // 40, E  # the oracle's rows take their time
+    l, _ = _logits(E + K, T, E)
+    g = torch.Generator().manual_seed(4)
+    ids = torch.argsort(torch.rand(T, E, generator=g), dim=1)[:, :K].to(torch.int32)
+    ids[torch.rand(T, K, generator=g) < 0.1] = -1
+    _check_backward(dev, l, ids, K, getattr(torch, dtype), score, renormalize, 2.5)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_backward_of_repeated_and_bad_ids(dev, score, renormalize):
+    """An expert twice in a row; ids outside; rows without any."""
+    import torch
+    l, _ = _logits(8, 6, 10)
+    ids = torch.tensor([[2, 2, 2], [0, 9, 0], [-1, -1, -1], [4, -1, 4], [10, 3, 1 << 30], [5, 6, 7]],
+                       dtype=torch.int32)
+    _check_backward(dev, l, ids, 3, torch.float32, score, renormalize, 1.0)
+
+
+def test_backward_leaves_gates_of_masked_pairs_out(dev):
+    """What stands in the gates and gradients of pairs without an expert does not matter."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    nan = math.nan
+    l, _ = _logits(3, 2, 6)
+    ids = torch.tensor([[1, -1], [-1, -1]], dtype=torch.int32, device=dev)
+    gates = torch.tensor([[0.5, nan], [nan, INF]], device=dev)
+    d = torch.tensor([[2.0, INF], [nan, nan]], device=dev)
+    for score in ("softmax", "sigmoid"):
+        for renormalize in (True, False):
+            dl = torch.full((2, 6), 9.0, device=dev)
+            p = B.make_route(2, 2, 6, score=score, renormalize=renormalize)
+            B.llep_route_backward(p, l.to(dev), ids, gates, d, dl)
+            assert bool(torch.isfinite(dl).all()) and not bool(dl[1].any())
+
+
+def test_backward_of_masked_logits(dev):
+    """Experts and rows of -infinity have no gradient."""
+    import torch
+    l, _ = _logits(6, 40, 24, masked=0.3)
+    for renormalize in (True, False):
+        ids, _ = oracle.route(l.numpy(), 4, renormalize=renormalize)
+        _, _, _, dl = _check_backward(dev, l, torch.from_numpy(ids).to(torch.int32), 4,
+                                      torch.float32, "softmax", renormalize, 1.0)
+        assert not bool(dl.cpu()[l == -INF].any())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_backward_against_differences(dev, score, renormalize):
+    """The kernel's gradient against differences of the kernel's gates: with steps of h = 2^-7 the
+    error of a central difference is h^2 / 6 times a third derivative (below 2 of these functions,
+    times the sum of |d gate|) and two gates' 64 u over 2 h."""
+    import torch
+    T, E, K, h = 3, 12, 3, 2.0 ** -7
+    l, _ = _logits(12, T, E)
+    l = (l * 1024).round() / 1024
+    p, x, _, ids, gates = _route(dev, l, K, score=score, renormalize=renormalize)
+    d = torch.randn(T, K, generator=torch.Generator().manual_seed(1))
+    _, _, _, dl = _check_backward(dev, l, ids.cpu(), K, torch.float32, score, renormalize, 1.0, d)
+    for e in range(E):
+        vals = []
+        for sign in (1, -1):
+            m = l.clone()
+            m[:, e] += sign * h
+            _, _, _, i2, g2 = _route(dev, m, K, score=score, renormalize=renormalize)
+            assert torch.equal(i2, ids)  # these logits are further apart than the steps
+            vals.append((g2.cpu().double() * d).sum(1))
+        want = (vals[0] - vals[1]) / (2 * h)
+        near = float(d.abs().sum(1).max()) * (h * h / 3 + 64 * U / h)
+        assert float((dl[:, e].cpu().double() - want).abs().max()) <= near
+
+
+# ---------------------------------------------------------------------------
+# calls
+# ---------------------------------------------------------------------------
+
+def test_no_tokens(dev):
+    import torch
+    from paper_2601_17111_amd.layer import Router
+    r = Router(0, 2, 8)
+    l = torch.empty((0, 8), device=dev)
+    ids, gates = r.forward(l)
+    assert ids.shape == (0, 2) and r.backward(l, gates).shape == (0, 8)
+
+
+def test_router_in_a_graph_and_on_a_stream(dev):
+    """Forward and backward captured, replayed with other logits; and on a stream of its own."""
+    import torch
+    from paper_2601_17111_amd.layer import Router
+    T, E, K = 50, 64, 4
+    ls = [_logits(i, T, E)[0].to(dev) for i in range(3)]
+    b = _logits(9, T, E)[1].to(dev)
+    d = torch.randn(T, K, device=dev)
+    r = Router(T, K, E, score="sigmoid", bias=b)
+    want = []
+    for l in ls:
+        ids, gates = r.forward(l)
+        want.append([t.clone() for t in (ids, gates, r.backward(l, d))])
+    x = ls[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r.forward(x)
+        out = r.backward(x, d)
+    for i in (1, 2, 0, 1):
+        x.copy_(ls[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, w) for a, w in zip((r.ids, r.gates, out), want[i]))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    r2 = Router(T, K, E, score="sigmoid", bias=b)
+    s.wait_stream(torch.cuda.current_stream())
+    ids, gates = r2.forward(ls[2], s)
+    out = r2.backward(ls[2], d, s)
+    s.synchronize()
+    assert all(torch.equal(a, w) for a, w in zip((ids, gates, out), want[2]))
+
+
+def test_same_bits_in_every_batch(dev):
+    """A row's ids and gates do not depend on the rows around it, nor on their number."""
+    import torch
+    l, b = _logits(21, 5000, 128)
+    for bias in (None, b):
+        _, _, _, ids, gates = _route(dev, l, 8, bias, score="sigmoid")
+        _, _, _, i1, g1 = _route(dev, l[4990:], 8, bias, score="sigmoid")
+        assert torch.equal(ids[4990:], i1) and torch.equal(gates[4990:], g1)
