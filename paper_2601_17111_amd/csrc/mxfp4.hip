@@ -9,7 +9,7 @@
 // it. Weights are packed (llep_pack_mxfp4) in blocks of 16 rows x one slice, 1 KB
 // each, 16 bytes of each row after another, so that lane l of a wavefront that
 // reads a block in order has its operand; the exponents of 16 rows lie in blocks
-// of four slices, 16 bytes a row.
+// of four slices, 64 bytes each, 4 bytes a row.
 #include <algorithm>
 #include <cmath>
 
@@ -157,7 +157,8 @@ hipError_t launch_dequantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const
 }
 
 // ---------------------------------------------------------------------------
-// packing: 16 bytes of a packed row, or its exponents in four slices, per thread
+// packing: 16 bytes of a packed row, or the exponents of four rows in a slice, per
+// thread
 // ---------------------------------------------------------------------------
 
 struct MxPackArgs {
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(MxPackArgs a) {
     const int64_t blk = at >> (is_data ? 6 : 4);
     const int cols = is_data ? a.nk : a.nq;
     const int kb = int(blk % cols);
-    int n = int(blk / cols) * 16 + (in & 15);
+    int n = int(blk / cols) * 16 + (is_data ? in & 15 : (in & 3) * 4);
     // two matrices: 32 rows of the first, then the matching 32 of the second
     const uint8_t *w = a.w0, *s = a.s0;
     if (a.w1) {
@@ -204,12 +205,13 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(MxPackArgs a) {
         }
       }
     } else {
-      const int blocks = (a.K + kBlockK - 1) / kBlockK;
-      const uint8_t *p = s + (e * a.N + (n < a.N ? n : 0)) * a.s_bytes;
+      const int blocks = (a.K + kBlockK - 1) / kBlockK, c0 = kb * 16 + (in >> 2) * 4;
 #pragma unroll
-      for (int b = 0; b < 16; ++b) {
-        const int c = kb * 16 + b;
-        v[b / 4] |= (n < a.N && c < blocks ? uint32_t(p[c]) : 127u) << (8 * (b % 4));
+      for (int r = 0; r < 4; ++r) {
+        const uint8_t *p = s + (e * a.N + min(n + r, a.N - 1)) * a.s_bytes;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          v[r] |= (n + r < a.N && c0 + b < blocks ? uint32_t(p[c0 + b]) : 127u) << (8 * b);
       }
     }
     reinterpret_cast<uint4 *>(a.out)[i] = make_uint4(v[0], v[1], v[2], v[3]);
@@ -304,7 +306,7 @@ __global__ __launch_bounds__(kWaves * kWave) void mx_stream_kernel(MxGemmArgs g)
     for (int n = 0; n < kNB; ++n) {  // and past the last block
       const uint32_t b = uint32_t(min(n, n_blk - 1 - blk0));
       offB[n] = b * uint32_t(g.b_blk_stride) + lane * 16;
-      offBs[n] = b * uint32_t(g.b_scale_blk_stride) + (lane & 15) * 16;
+      offBs[n] = b * uint32_t(g.b_scale_blk_stride) + (lane & 15) * 4;
     }
     f32x4 acc[kMB][kNB];
 #pragma unroll
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(kWaves * kWave) void mx_stream_kernel(MxGemmArgs g)
 #pragma unroll
         for (int n = 0; n < kNB; ++n) {
           fb[u][n] = *reinterpret_cast<const i32x4 *>(B + int64_t(k) * 1024 + offB[n]);
-          sb[u][n] = *reinterpret_cast<const int32_t *>(Bs + (k >> 2) * 256 + (k & 3) * 4 + offBs[n]);
+          sb[u][n] = *reinterpret_cast<const int32_t *>(Bs + k * 64 + offBs[n]);
         }
 #pragma unroll
         for (int m = 0; m < kMB; ++m) {
