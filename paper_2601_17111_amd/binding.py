@@ -802,21 +802,31 @@ def llep_mxfp4_scale_bytes(D: int) -> int:
     return n
 
 
+def _mxfp4_bytes(D: int):
+    """(llep_mxfp4_row_bytes(D), llep_mxfp4_scale_bytes(D))"""
+    slices = (D + 127) >> 7
+    if 1 <= D <= LLEP_MAX_FFN_DIM:
+        return slices * 64, (slices + 3 >> 2) * 16
+    return llep_mxfp4_row_bytes(D), llep_mxfp4_scale_bytes(D)
+
+
 def _byte_rows(what: str, t, R: int, least: int) -> int:
     """The bytes from one row of t to the next: t [R, >= least] uint8 on the GPU, whose rows may be
     parts of longer ones (a view of a buffer's columns)."""
     import torch
     if t.dtype is not torch.uint8:
         raise TypeError(f"{what} is {t.dtype}, not {torch.uint8}")
-    if t.dim() != 2 or t.shape[0] != R or t.shape[1] < least:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, not [{R}, {least}] or wider")
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != R or shape[1] < least:
+        raise ValueError(f"{what} has shape {tuple(shape)}, not [{R}, {least}] or wider")
     if not t.is_cuda:
         raise ValueError(f"{what} is not on a GPU")
     if R <= 1:  # the stride of an only row means nothing
-        return (t.shape[1] + 15) // 16 * 16
-    if t.stride(1) != 1 or t.stride(0) < t.shape[1]:
+        return (shape[1] + 15) // 16 * 16
+    pitch, step = t.stride()
+    if step != 1 or pitch < shape[1]:
         raise ValueError(f"{what} is not made of rows of bytes")
-    return t.stride(0)
+    return pitch
 
 
 def llep_quantize_rows_mxfp4(x, q, scale, stream=None):
@@ -825,8 +835,9 @@ def llep_quantize_rows_mxfp4(x, q, scale, stream=None):
     R, D = x.shape
     code = _dtype_code(x)
     _dense("x", x, (R, D), x.dtype)
-    q_pitch = _byte_rows("q", q, R, llep_mxfp4_row_bytes(D))
-    s_pitch = _byte_rows("scale", scale, R, llep_mxfp4_scale_bytes(D))
+    q_bytes, s_bytes = _mxfp4_bytes(D)
+    q_pitch = _byte_rows("q", q, R, q_bytes)
+    s_pitch = _byte_rows("scale", scale, R, s_bytes)
     _here(x, q, scale)
     _check(lib().llep_quantize_rows_mxfp4(R, D, code, _ptr(x), _ptr(q), q_pitch, _ptr(scale),
                                           s_pitch, _stream(stream)), "llep_quantize_rows_mxfp4")
@@ -837,8 +848,9 @@ def llep_dequantize_rows_mxfp4(q, scale, out, stream=None):
     R, D = out.shape
     code = _dtype_code(out)
     _dense("out", out, (R, D), out.dtype)
-    q_pitch = _byte_rows("q", q, R, llep_mxfp4_row_bytes(D))
-    s_pitch = _byte_rows("scale", scale, R, llep_mxfp4_scale_bytes(D))
+    q_bytes, s_bytes = _mxfp4_bytes(D)
+    q_pitch = _byte_rows("q", q, R, q_bytes)
+    s_pitch = _byte_rows("scale", scale, R, s_bytes)
     _here(q, scale, out)
     _check(lib().llep_dequantize_rows_mxfp4(R, D, code, _ptr(q), q_pitch, _ptr(scale), s_pitch,
                                             _ptr(out), _stream(stream)),
@@ -881,9 +893,10 @@ def llep_mxfp4_matmul(x, x_scale, w_packed, out, K: int, stream=None):
     import torch
     M, N = out.shape
     code = _dtype_code(out)
-    q_pitch = _byte_rows("x", x, M, llep_mxfp4_row_bytes(K))
-    s_pitch = _byte_rows("x_scale", x_scale, M, llep_mxfp4_scale_bytes(K))
-    _dense("w_packed", w_packed, (1, lib().llep_packed_mxfp4_bytes(1, N, K)), torch.uint8)
+    q_bytes, s_bytes = _mxfp4_bytes(K)
+    q_pitch = _byte_rows("x", x, M, q_bytes)
+    s_pitch = _byte_rows("x_scale", x_scale, M, s_bytes)
+    _dense("w_packed", w_packed, (1, (N + 15) // 16 * 16 * (q_bytes + s_bytes)), torch.uint8)
     _dense("out", out, (M, N), out.dtype)
     _here(x, x_scale, w_packed, out)
     _check(lib().llep_mxfp4_matmul(M, N, K, _ptr(x), q_pitch, _ptr(x_scale), s_pitch,
