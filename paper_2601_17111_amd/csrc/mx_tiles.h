@@ -12,9 +12,12 @@
 // with words next to each other, requested as words or written by the scale waves,
 // the products took 3 to 6% longer.)
 //
-// What bounds them: 8192^3 takes 262 us, 4.2 PFLOP/s; the matrix instructions are at
+// What bounds them: 8192^3 takes 258 us, 4.3 PFLOP/s; the matrix instructions are at
 // work 61% of the time, at the 1.6 GHz that the chip's power leaves (of 2.4: matrix
-// instructions alone, on random operands, reach 6.2 PFLOP/s).
+// instructions alone, on random operands, reach 6.2 PFLOP/s). A tile's epilogue is
+// 4.5 us of 21 (K = 2048). Requests into the L2 four to eight slices further ahead made
+// products 5 to 10% slower, half tiles in a last round that leaves workgroups idle were
+// no faster.
 #pragma once
 
 #include "gemm.h"
@@ -176,14 +179,6 @@ __device__ __forceinline__ void mx_tiles(const MxGemmArgs g, char *smem, TileCoo
   };
   setup(t);
   prologue();
-  // Stores of the last epilogue that may still be under way behind the first
-  // slices' requests (counted with them, in the order of issue): kStores, or none
-  // that is counted on. The memory takes all compute units' outputs at once while
-  // the next tile's first slices are worked on; waiting for it here cost 6.8 us a
-  // tile (of 21, 8192 x 7168 x 2048).
-  constexpr int kStores = kEpi == kMxSwiglu ? 2 * TM : kEpi == kMxF32 ? 4 * TM * TN : 2 * TM * TN;
-  int behind = 0;
-
   using Frag = i32x4;
   auto read_a = [&](int st, int ks, int i) {
     const int row = wm * WM + i * 32 + (lane & 31), kc = ks * 2 + h;
@@ -277,30 +272,14 @@ __device__ __forceinline__ void mx_tiles(const MxGemmArgs g, char *smem, TileCoo
     const int active =
         __builtin_amdgcn_readfirstlane(int(t.rows_valid > wm * WM && t.cols_valid > wn * WN));
     // slice 0, and the first exponents
-    const bool late = behind != 0 && nk >= kMxAhead;
-    behind = 0;
-    if (dma && late)
-      wait_vmcnt<(kMxAhead - 1) * PER_STAGE + kStores>();
-    else if (dma && nk >= kMxAhead)
+    // (behind a tile's stores, which are waited for as well: counted past, 8192 x 8192 x
+    // 2048 took 87 us for 84)
+    if (dma && nk >= kMxAhead)
       wait_vmcnt<(kMxAhead - 1) * PER_STAGE>();
-    else if (late)
-      wait_vmcnt<kStores>();
     else
       wait_vmcnt<0>();
     wait_and_sync<63>();
     int st = 0, kt = 0, st_req = kMxAhead % kMxStages;
-    // a DMA wave at the barrier before slice kt + 1 (1 and 2 were requested before
-    // the stores)
-    // (hidden from the compiler, which would peel these turns off the loop and
-    // keep the accumulators twice)
-    int grace = __builtin_amdgcn_readfirstlane(late ? kMxAhead - 1 : 0);
-    auto wait_slice = [&](int) {
-      if (--grace >= 0)
-        wait_vmcnt<(kMxAhead - 2) * PER_STAGE + D0 + kStores>();
-      else
-        wait_vmcnt<(kMxAhead - 2) * PER_STAGE + D0>();
-      wait_and_sync<63>();
-    };
     // the whole of k, one copy for the DMA waves and one for the others
     auto work = [&](auto dma_wave) {
       constexpr bool kDma = decltype(dma_wave)::value;
@@ -323,10 +302,12 @@ __device__ __forceinline__ void mx_tiles(const MxGemmArgs g, char *smem, TileCoo
         if (!kDma && (kt & 3) == 0 && kt + 4 < nk) request_scales((kt >> 2) + 1);
         step(sel0, dma_wave, std::false_type{}, acc, fa, fb0, sc, fb1, raw, st, kt, st_req,
              kt + kMxAhead);
-        if (kDma)
-          wait_slice(kt);
-        else
+        if (kDma) {
+          wait_vmcnt<(kMxAhead - 2) * PER_STAGE + D0>();
+          wait_and_sync<63>();
+        } else {
           wait_scales(kt);
+        }
         st = next_stage(st);
         step(sel2, dma_wave, std::true_type{}, acc, fa, fb1, sc, fb0, raw, st, kt + 1, st_req,
              kt + kMxAhead);
@@ -483,9 +464,6 @@ __device__ __forceinline__ void mx_tiles(const MxGemmArgs g, char *smem, TileCoo
       }
     }
     if (!more) break;
-    // a whole part of a tile: all of its stores were issued (those of rows that are
-    // stored from the registers are not counted)
-    if (rows_w >= WM && ncol0 + WN <= g.N && all_staged) behind = 1;
   }
 }
 
