@@ -414,7 +414,9 @@ __device__ __forceinline__ void mx_tiles(const MxGemmArgs g, char *smem, TileCoo
       }
     } else {
       // rows of whole 16-byte vectors go through the staging area, 32 rows at a
-      // time, as runs of a row; others from the registers
+      // time, as runs of a row; others from the registers. Stores go past the caches (a
+      // product and a read of its outputs: 16384 x 4096 x 1024 105 -> 97 us, 32768 x 7168 x
+      // 1024 in float32 559 -> 535, but 8192 x 7168 x 2048 120 -> 124)
       constexpr bool kF32 = kEpi == kMxF32;
       const bool staged = all_staged;
       // columns of a piece: its rows are 128 bytes, whose 16-byte chunks are

@@ -43,21 +43,45 @@ struct MxRowsArgs {
 
 constexpr int kMxRowWaves = 4;
 
-template <typename T, bool kOdd>
+// A wavefront's items (row, part of it), one after another
+struct MxRowItems {
+  int64_t row, rows_on;
+  int part, parts_on, parts;
+  __device__ __forceinline__ explicit MxRowItems(int D) {
+    parts = (D + 511) / 512;
+    const uint32_t first = blockIdx.x * kMxRowWaves +
+                           __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t step = gridDim.x * kMxRowWaves;
+    row = first / uint32_t(parts), part = int(first % uint32_t(parts));
+    rows_on = step / uint32_t(parts), parts_on = int(step % uint32_t(parts));
+  }
+  __device__ __forceinline__ void next() {
+    row += rows_on, part += parts_on;
+    if (part >= parts) part -= parts, ++row;
+  }
+};
+
+// kOnce: more than the 256 MB cache behind the L2s, which loads and stores go past
+// (92160 x 2880 132 -> 119 us, and 136 -> 101 for the values back). With less, the call
+// that reads the results takes longer for it than these save (8192 x 2880 and 2880 x
+// 2880 weights 63 -> 71; values back and a read of them 26.7 -> 28.4).
+template <typename T, bool kOdd, bool kOnce>
 __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRowsArgs a) {
   const int lane = lane_id();
-  const int parts = (a.D + 511) / 512, q_bytes = (a.D + kSliceK - 1) / kSliceK * 64;
-  const int64_t items = a.R * parts;
-  for (int64_t i = int64_t(blockIdx.x) * kMxRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-       i < items; i += int64_t(gridDim.x) * kMxRowWaves) {
-    const int64_t row = i / parts;
-    const int part = int(i - row * parts), c = part * 512 + lane * 8;
+  const int q_bytes = (a.D + kSliceK - 1) / kSliceK * 64;
+  for (MxRowItems it(a.D); it.row < a.R; it.next()) {
+    const int64_t row = it.row;
+    const int part = it.part, c = part * 512 + lane * 8;
     RawVec<T, 8> in;
     in.zero();
     if (c < a.D) {
       const T *p = static_cast<const T *>(a.x) + row * a.D + c;
       if constexpr (kOdd)
         in.load_any(p, a.D - c);
+      else if constexpr (kOnce)
+#pragma unroll
+        for (int j = 0; j < RawVec<T, 8>::kWords; ++j)
+          in.w[j] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(p) + j);
       else
         in.load(p);
     }
@@ -68,10 +92,15 @@ __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRows
     most = max(most, dpp<0x4e, 0xf>(most));
     const uint32_t e = mx_exponent(most);
     const float step = mx_step(e);
-    if (c / 2 < q_bytes)
-      *reinterpret_cast<uint32_t *>(a.q + row * a.q_pitch + c / 2) =
-          mx_pack4(in[0], in[1], in[2], in[3], step) |
-          (mx_pack4(in[4], in[5], in[6], in[7], step) << 16);
+    if (c / 2 < q_bytes) {
+      const uint32_t v = mx_pack4(in[0], in[1], in[2], in[3], step) |
+                         (mx_pack4(in[4], in[5], in[6], in[7], step) << 16);
+      uint32_t *to = reinterpret_cast<uint32_t *>(a.q + row * a.q_pitch + c / 2);
+      if constexpr (kOnce)
+        __builtin_nontemporal_store(v, to);
+      else
+        *to = v;
+    }
     uint32_t w = e | (dpp<0x104, 0xf>(e) << 8);  // row_shl:4, :8: four blocks of 16 lanes
     w |= dpp<0x108, 0xf>(w) << 16;
     if ((lane & 15) == 0)
@@ -79,46 +108,65 @@ __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRows
   }
 }
 
-template <typename T>
+// kN values of a lane at a time, so that a wavefront's stores are whole pieces of the
+// row: 8 of bfloat16, 4 of float32 (20000 x 7168 175 -> 147 us).
+template <typename T, bool kOnce>
 __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_dequantize_kernel(MxRowsArgs a) {
+  constexpr int kN = 16 / sizeof(T);
+  using Word = std::conditional_t<kN == 8, uint32_t, uint16_t>;
   const int lane = lane_id();
-  const int parts = (a.D + 511) / 512;
-  const int64_t items = a.R * parts;
   const bool whole = a.D % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
-  for (int64_t i = int64_t(blockIdx.x) * kMxRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-       i < items; i += int64_t(gridDim.x) * kMxRowWaves) {
-    const int64_t row = i / parts;
-    const int c = int(i - row * parts) * 512 + lane * 8;
-    if (c >= a.D) continue;
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(a.q + row * a.q_pitch + c / 2);
-    const uint32_t e = a.scale[row * a.s_pitch + c / kBlockK];
-    // 2^-127 is below the normal range: half of it times two
-    const float step = e == 0 ? 0x1p-126f : mx_step(e);
-    float v[8];
+  for (MxRowItems it(a.D); it.row < a.R; it.next()) {
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      const auto two = j == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 0)
-                       : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 1)
-                       : j == 4 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 2)
-                                : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 3);
-      v[j] = two[0], v[j + 1] = two[1];
-    }
+    for (int part = 0; part < 8 / kN; ++part) {
+      const int c = it.part * 512 + (part * kWave + lane) * kN;
+      if (c >= a.D) continue;
+      const uint32_t w = *reinterpret_cast<const Word *>(a.q + it.row * a.q_pitch + c / 2);
+      const uint32_t e = a.scale[it.row * a.s_pitch + c / kBlockK];
+      // 2^-127 is below the normal range: half of it times two
+      const float step = e == 0 ? 0x1p-126f : mx_step(e);
+      float v[kN];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (e == 0) v[j] *= 0.5f;
-      if (e == 255) v[j] = __uint_as_float(0x7fc00000u);
+      for (int j = 0; j < kN; j += 2) {
+        const auto two = j == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 0)
+                         : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 1)
+                         : j == 4 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 2)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, step, 3);
+        v[j] = two[0], v[j + 1] = two[1];
+      }
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        if (e == 0) v[j] *= 0.5f;
+        if (e == 255) v[j] = __uint_as_float(0x7fc00000u);
+      }
+      T *p = static_cast<T *>(a.out) + it.row * a.D + c;
+      if (whole) {
+        i32x4 u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (kN == 8)
+            u[j] = int32_t(pack_bf16x2(v[2 * j], v[2 * j + 1]));
+          else
+            u[j] = __float_as_int(v[j]);
+        }
+        if constexpr (kOnce)
+          __builtin_nontemporal_store(u, reinterpret_cast<i32x4 *>(p));
+        else
+          *reinterpret_cast<i32x4 *>(p) = u;
+      } else {
+        store_any<T, kN>(p, v, a.D - c);
+      }
     }
-    T *p = static_cast<T *>(a.out) + row * a.D + c;
-    if (whole)
-      store_vec<T, 8>(p, v);
-    else
-      store_any<T, 8>(p, v, a.D - c);
   }
 }
 
 static dim3 mx_rows_grid(const MxRowsArgs &a) {
   const int64_t items = a.R * ((a.D + 511) / 512);
   return dim3(uint32_t(std::min<int64_t>((items + kMxRowWaves - 1) / kMxRowWaves, 256 * 8 * 4)));
+}
+
+static bool mx_rows_once(int64_t R, int32_t D, llep_dtype dtype) {
+  return R * D * (dtype == LLEP_BF16 ? 2 : 4) > (int64_t(256) << 20);
 }
 
 hipError_t launch_quantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const void *x, uint8_t *q,
@@ -129,15 +177,17 @@ hipError_t launch_quantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const v
   const bool whole = D % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
   const dim3 grid = mx_rows_grid(a), threads(kMxRowWaves * kWave);
   if (dtype == LLEP_BF16) {
-    if (whole)
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false>), grid, threads, 0, stream, a);
+    if (whole && mx_rows_once(R, D, dtype))
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, true>), grid, threads, 0, stream, a);
+    else if (whole)
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, false>), grid, threads, 0, stream, a);
     else
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, true>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, true, false>), grid, threads, 0, stream, a);
   } else {
     if (whole)
-      hipLaunchKernelGGL((mx_quantize_kernel<float, false>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<float, false, false>), grid, threads, 0, stream, a);
     else
-      hipLaunchKernelGGL((mx_quantize_kernel<float, true>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<float, true, false>), grid, threads, 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -149,10 +199,18 @@ hipError_t launch_dequantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const
   const MxRowsArgs a = {R,   D, q_pitch, s_pitch, nullptr, out, const_cast<uint8_t *>(q),
                         const_cast<uint8_t *>(scale)};
   const dim3 grid = mx_rows_grid(a), threads(kMxRowWaves * kWave);
-  if (dtype == LLEP_BF16)
-    hipLaunchKernelGGL((mx_dequantize_kernel<uint16_t>), grid, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL((mx_dequantize_kernel<float>), grid, threads, 0, stream, a);
+  const bool once = mx_rows_once(R, D, dtype);
+  if (dtype == LLEP_BF16) {
+    if (once)
+      hipLaunchKernelGGL((mx_dequantize_kernel<uint16_t, true>), grid, threads, 0, stream, a);
+    else
+      hipLaunchKernelGGL((mx_dequantize_kernel<uint16_t, false>), grid, threads, 0, stream, a);
+  } else {
+    if (once)
+      hipLaunchKernelGGL((mx_dequantize_kernel<float, true>), grid, threads, 0, stream, a);
+    else
+      hipLaunchKernelGGL((mx_dequantize_kernel<float, false>), grid, threads, 0, stream, a);
+  }
   return hipGetLastError();
 }
 

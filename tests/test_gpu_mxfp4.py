@@ -228,7 +228,7 @@ def test_products(dev, M, N, K):
     (2500, 4104, 200), (1024, 1024, 768), (1025, 2050, 1300), (600, 5000, 3001),
     # 256-row tiles, several of them for a workgroup
     (8192, 4096, 128), (8200, 4097, 257), (6001, 5008, 500), (3000, 7001, 1000), (4100, 4100, 2890),
-    (16385, 2056, 400),
+    (16385, 2056, 400), (16400, 6208, 130),
 ])
 def test_products_of_many_rows(dev, M, N, K):
     _check_product(dev, M, N, K, M + N + K)
@@ -322,6 +322,25 @@ def test_outputs_past_32_bits(dev):
     xv, wv = torch.from_numpy(xv).to(dev), torch.from_numpy(wv).to(dev)
     for a, b in ((0, 300), (M // 2, M // 2 + 300), (M - 300, M)):
         assert torch.equal(out[a:b], (xv[a:b] @ wv.t()).bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_of_more_than_the_cache(dev, dtype):
+    """Rows of more than 256 MB: the same as those of smaller calls, and their values."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    R, D = 50001, 2888
+    x = torch.randn(R, D, device=dev).to(getattr(torch, dtype))
+    assert x.numel() * x.element_size() > 256 << 20
+    q, s = _quantize(dev, x)
+    out = torch.empty_like(x)
+    B.llep_dequantize_rows_mxfp4(q, s, out)
+    for a, b in ((0, 7000), (25000, 32000), (43000, R)):
+        q1, s1 = _quantize(dev, x[a:b].clone())
+        assert torch.equal(q[a:b], q1) and torch.equal(s[a:b], s1)
+        part = torch.empty_like(x[a:b])
+        B.llep_dequantize_rows_mxfp4(q1, s1, part)
+        assert torch.equal(out[a:b], part)
 
 
 def test_packed_gate_and_up_rows(dev):
