@@ -821,9 +821,9 @@ def _byte_rows(what: str, t, R: int, least: int) -> int:
         raise ValueError(f"{what} has shape {tuple(shape)}, not [{R}, {least}] or wider")
     if not t.is_cuda:
         raise ValueError(f"{what} is not on a GPU")
-    if R <= 1:  # the stride of an only row means nothing
-        return (shape[1] + 15) // 16 * 16
     pitch, step = t.stride()
+    if R <= 1:  # the stride of an only row means nothing
+        pitch = (shape[1] + 15) // 16 * 16
     if step != 1 or pitch < shape[1]:
         raise ValueError(f"{what} is not made of rows of bytes")
     return pitch

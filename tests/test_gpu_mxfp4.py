@@ -226,12 +226,34 @@ def test_products(dev, M, N, K):
     # columns, odd rows and columns, fewer tiles than workgroups and more
     (1800, 1800, 64), (1793, 1801, 130), (130, 30001, 70), (1500, 3001, 501), (2050, 1288, 640),
     (2500, 4104, 200), (1024, 1024, 768), (1025, 2050, 1300), (600, 5000, 3001),
-    # 256-row tiles, several of them for a workgroup
+    # 256-row tiles, several of them for a workgroup, and those that are just not
     (8192, 4096, 128), (8200, 4097, 257), (6001, 5008, 500), (3000, 7001, 1000), (4100, 4100, 2890),
-    (16385, 2056, 400), (16400, 6208, 130),
+    (16385, 2056, 400), (16400, 6208, 130), (8190, 8185, 333), (7937, 8200, 1500), (4090, 4090, 2890),
+    (12200, 5377, 1000), (8100, 8100, 64),
 ])
 def test_products_of_many_rows(dev, M, N, K):
     _check_product(dev, M, N, K, M + N + K)
+
+
+@pytest.mark.parametrize("M,N,K,form", [
+    (1, 7168, 2048, "stream_kernel<1, 1, 8"), (16, 300, 65, "stream_kernel<1, 1, 8"),
+    (17, 768, 2048, "stream_kernel<2, 1, 16"), (64, 2048, 7168, "stream_kernel<2, 1, 16"),
+    (64, 7168, 2048, "stream_kernel<2, 2, 8"), (33, 20000, 130, "tiles_kernel<128"), (40, 7168, 1000, "stream_kernel<2, 2, 8"),
+    (256, 4096, 4096, "stream_kernel<4, 4, 8"), (200, 4200, 5000, "tiles_kernel<128"), (200, 4000, 5000, "stream_kernel<4, 4, 8"),
+    (1024, 7168, 2048, "tiles_kernel<128"), (2050, 1288, 640, "tiles_kernel<128"),
+    (8192, 4096, 128, "tiles_kernel<256"), (4100, 4100, 2890, "tiles_kernel<128"),
+    (4090, 4090, 2890, "tiles_kernel<256"), (8190, 8185, 333, "tiles_kernel<256"),
+])
+def test_forms(dev, M, N, K, form):
+    """Each of the ways that a product can take, by the name of its kernel, gives whole numbers."""
+    import torch
+    from torch.profiler import ProfilerActivity, profile
+    torch.cuda.synchronize()
+    with profile(activities=[ProfilerActivity.CUDA]) as seen:
+        _check_product(dev, M, N, K, M + N + K)
+        torch.cuda.synchronize()
+    names = {e.key for e in seen.key_averages() if "llep::mx_" in e.key and "pack" not in e.key}
+    assert names and all(form in n for n in names), names
 
 
 @pytest.mark.parametrize("M,N,K", [(5, 300, 1000), (40, 200, 2880), (700, 1500, 2880), (2900, 3000, 300)])
@@ -252,7 +274,7 @@ def test_products_of_many_exponents(dev, M, N, K):
         assert bool(((out.double() - want).abs() <= tol).all())
 
 
-@pytest.mark.parametrize("M,N", [(4, 70), (40, 300), (100, 300), (1500, 1500), (4100, 4100)])
+@pytest.mark.parametrize("M,N", [(4, 70), (40, 300), (100, 300), (1500, 1500), (4100, 4100), (4090, 4090)])
 def test_blocks_of_nan(dev, M, N):
     """An exponent of 255 makes the rows that have it NaN, and no others."""
     import torch
@@ -293,7 +315,7 @@ def test_rows_of_a_product_lie_apart(dev):
     from paper_2601_17111_amd import binding as B
     g = np.random.default_rng(5)
     K, N = 700, 1800
-    for M in (3, 30, 200, 1800):
+    for M in (3, 30, 200, 1800, 8190):
         xc, xe, xv = _random_rows(g, M, K, 126, 129)
         wc, we, wv = _random_rows(g, N, K, 126, 129)
         q, s = _as_rows(dev, xc, xe)
@@ -440,6 +462,7 @@ def test_refusals(dev):
         (lambda: B.llep_quantize_rows_mxfp4(x, torch.zeros((4, 80), **u8)[:, 8:72], s), B.LLEPError),
         (lambda: B.llep_quantize_rows_mxfp4(x, torch.zeros((64, 4), **u8).t(), s), ValueError),
         (lambda: B.llep_quantize_rows_mxfp4(x, q[:1].expand(4, 64), s), ValueError),
+        (lambda: B.llep_quantize_rows_mxfp4(x[:1], torch.zeros((1, 128), **u8)[:, ::2], s[:1]), ValueError),
         (lambda: B.llep_quantize_rows_mxfp4(torch.zeros((4, 0), device=dev), q, s), B.LLEPError),
         (lambda: B.llep_dequantize_rows_mxfp4(q, s, x.half()), TypeError),
         (lambda: B.llep_dequantize_rows_mxfp4(q, s, torch.zeros((4, 200), device=dev)), ValueError),

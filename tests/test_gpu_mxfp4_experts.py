@@ -248,6 +248,32 @@ def test_router_and_block_training(dev):
         assert (np.abs(dl.double().cpu().numpy() - want) <= near).all()
 
 
+def test_allocations_are_the_streams_own(dev):
+    """What calls with stream= allocate is that stream's."""
+    import torch
+    from paper_2601_17111_amd.layer import Mxfp4Experts, Router
+    from test_gpu_stream_buffers import _stream_of, _tensors
+    c = Case(dev, 37, "bf16", "channel", seed=3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    layer = c.block.layer
+    router = Router(c.T, layer.K, layer.E)
+    l = torch.randn(c.T, layer.E, device=dev)
+    side.wait_stream(torch.cuda.current_stream())
+    here = {**_tensors(layer), **_tensors(router), **_tensors(c.block)}
+    experts = Mxfp4Experts.from_weights(*c.w, stream=side)
+    ids, gates = router.forward(l, side)
+    layer.forward_mxfp4(ids, gates, c.x, experts, stream=side)
+    c.block.forward_mxfp4(ids, gates, c.x, experts, stream=side)
+    router.backward(l, gates, side)
+    side.synchronize()
+    made = {**_tensors(layer), **_tensors(router), **_tensors(c.block), **_tensors(experts)}
+    made = {k: t for k, t in made.items() if k not in here}
+    assert len(made) >= 7
+    for k, t in made.items():
+        assert _stream_of(t) == side.cuda_stream, k
+
+
 def test_no_tokens(dev):
     import torch
     from paper_2601_17111_amd.layer import LLEPLayer

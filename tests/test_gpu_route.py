@@ -191,6 +191,52 @@ def test_large_logits(dev):
     _check(dev, l * 1000, 2, score="softmax")
 
 
+@pytest.mark.parametrize("E,G", [(40, 1), (256, 8), (300, 1)])
+def test_infinite_biases(dev, E, G):
+    """A bias of infinity is taken first, of minus infinity or NaN never, in few and many rows."""
+    import torch
+    how = dict(groups=G, top_groups=G // 2, group_score="top2") if G > 1 else {}
+    for T in (5, 1100):
+        l, b = _logits(E, T, E, masked=0.1)
+        b[3::17], b[5::11], b[8::13] = INF, -INF, math.nan
+        rows = slice(0, None, 1 if T < 10 else 50)
+        for K in (4, 8):
+            for score in ("softmax", "sigmoid"):
+                _, x, _, ids, _ = _route(dev, l, K, b, score=score, **how)
+                want, _ = oracle.route(l.numpy()[rows], K, bias=b.numpy(), score=score, **how)
+                assert np.array_equal(ids.cpu().numpy()[rows], want)
+
+
+def test_offsets_past_32_bits(dev):
+    """More than 2^31 logits, with and without a bias, and their gradients: the last rows as in a
+    call of their own."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    T, E, K, n = (1 << 22) + 300, 512, 8, 700
+    x = torch.empty((T, E), dtype=torch.bfloat16, device=dev).normal_()
+    assert x.numel() > 2 ** 31
+    b = torch.randn(E, device=dev) * 0.1
+    d = torch.randn(T, K, device=dev)
+    last = x[-n:].clone()
+    for bias in (None, b):
+        outs = []
+        for y, dy in ((x, d), (last, d[-n:].clone())):
+            p = B.make_route(len(y), K, E, score="sigmoid")
+            ids = torch.empty((len(y), K), dtype=torch.int32, device=dev)
+            gates = torch.empty((len(y), K), device=dev)
+            B.llep_route(p, y, bias, ids, gates)
+            dl = torch.empty_like(y)
+            B.llep_route_backward(p, y, ids, gates, dy, dl)
+            outs.append((ids[-n:], gates[-n:], dl[-n:]))
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][0], outs[1][0])
+        # (few and many rows add up in another order: each within 64 u, of gradients 200 + 2 K)
+        near = 2 * 64 * U * outs[1][1].abs()
+        assert bool(((outs[0][1] - outs[1][1]).abs() <= near).all())
+        near = 2 * (216 * U * float(d.abs().max()) * (1 + K) + 2.0 ** -8 * outs[1][2].float().abs())
+        assert bool(((outs[0][2].float() - outs[1][2].float()).abs() <= near).all())
+
+
 def test_unaligned_rows_and_neighbours(dev):
     """Logits that start at any element; nothing beyond the outputs is written."""
     import torch
