@@ -735,6 +735,40 @@ def _here(*tensors):
             raise ValueError(f"a tensor is on {t.device}, the current device is {current}")
 
 
+_torch = None  # the module, once a call below has needed it (an import statement is 0.2 us)
+
+
+def _type_code(t):
+    """_dtype_code(t), and torch."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    dtype = t.dtype
+    return (LLEP_BF16 if dtype is _torch.bfloat16 else
+            LLEP_F32 if dtype is _torch.float32 else _dtype_code(t)), _torch
+
+
+def _arguments(stream, *specs):
+    """The call's stream, if all of the specs (what, tensor or None, shape, dtype) are dense tensors
+    on the current device; refuses others as _dense and _here do. In one pass: a call for one token
+    takes the GPU 3 to 6 us."""
+    dev = specs[0][1].get_device()
+    for _, t, shape, dtype in specs:
+        if t is not None and (t.get_device() != dev or t.dtype is not dtype or t.shape != shape
+                              or not t.is_contiguous()):
+            break
+    else:
+        if dev >= 0 and _torch._C._cuda_getDevice() == dev:
+            if stream is not None:
+                return stream.cuda_stream
+            return _torch._C._cuda_getCurrentRawStream(dev)
+    for what, t, shape, dtype in specs:
+        _dense(what, t, shape, dtype)
+    _here(*(t for _, t, _, _ in specs))
+    return _stream(stream)
+
+
 def make_route(T: int, K: int, E: int, score: str = "softmax", groups: int = 1,
                top_groups: int = 1, group_score: str = "max", renormalize: bool = True,
                scale: float = 1.0) -> llep_route_params:
@@ -754,34 +788,31 @@ def make_route(T: int, K: int, E: int, score: str = "softmax", groups: int = 1,
 def llep_route(params: llep_route_params, logits, bias, ids, gates, stream=None):
     """Router logits [T, E] (bf16 or float32) to ids [T, K] int32 and gates [T, K] float32 (see
     llep.h); bias [E] float32 or None."""
-    import torch
     T, K, E = params.T, params.K, params.E
-    code = _dtype_code(logits)
-    _dense("logits", logits, (T, E), logits.dtype)
-    _dense("bias", bias, (E,), torch.float32)
-    _dense("ids", ids, (T, K), torch.int32)
-    _dense("gates", gates, (T, K), torch.float32)
-    _here(logits, bias, ids, gates)
-    _check(lib().llep_route(ctypes.byref(params), code, _ptr(logits), _ptr(bias), _ptr(ids),
-                            _ptr(gates), _stream(stream)), "llep_route")
+    code, torch = _type_code(logits)
+    at = _arguments(stream, ("logits", logits, (T, E), logits.dtype),
+                    ("bias", bias, (E,), torch.float32), ("ids", ids, (T, K), torch.int32),
+                    ("gates", gates, (T, K), torch.float32))
+    rc = lib().llep_route(ctypes.byref(params), code, logits.data_ptr(), _ptr(bias),
+                          ids.data_ptr(), gates.data_ptr(), at)
+    if rc:
+        _check(rc, "llep_route")
 
 
 def llep_route_backward(params: llep_route_params, logits, ids, gates, d_gates, d_logits,
                         stream=None):
     """d_logits [T, E] (bf16 or float32) from d_gates [T, K] float32 and llep_route's inputs and
     outputs; logits (of d_logits' type) may be None for the renormalized softmax."""
-    import torch
     T, K, E = params.T, params.K, params.E
-    code = _dtype_code(d_logits)
-    _dense("logits", logits, (T, E), d_logits.dtype)
-    _dense("ids", ids, (T, K), torch.int32)
-    _dense("gates", gates, (T, K), torch.float32)
-    _dense("d_gates", d_gates, (T, K), torch.float32)
-    _dense("d_logits", d_logits, (T, E), d_logits.dtype)
-    _here(logits, ids, gates, d_gates, d_logits)
-    _check(lib().llep_route_backward(ctypes.byref(params), code, _ptr(logits), _ptr(ids),
-                                     _ptr(gates), _ptr(d_gates), _ptr(d_logits),
-                                     _stream(stream)), "llep_route_backward")
+    code, torch = _type_code(d_logits)
+    at = _arguments(stream, ("d_logits", d_logits, (T, E), d_logits.dtype),
+                    ("logits", logits, (T, E), d_logits.dtype), ("ids", ids, (T, K), torch.int32),
+                    ("gates", gates, (T, K), torch.float32),
+                    ("d_gates", d_gates, (T, K), torch.float32))
+    rc = lib().llep_route_backward(ctypes.byref(params), code, _ptr(logits), ids.data_ptr(),
+                                   gates.data_ptr(), d_gates.data_ptr(), d_logits.data_ptr(), at)
+    if rc:
+        _check(rc, "llep_route_backward")
 
 
 # ---- 4-bit rows and products ---------------------------------------------------------
@@ -810,17 +841,16 @@ def _mxfp4_bytes(D: int):
     return llep_mxfp4_row_bytes(D), llep_mxfp4_scale_bytes(D)
 
 
-def _byte_rows(what: str, t, R: int, least: int) -> int:
-    """The bytes from one row of t to the next: t [R, >= least] uint8 on the GPU, whose rows may be
+def _byte_rows(what: str, t, R: int, least: int, dev: int) -> int:
+    """The bytes from one row of t to the next: t [R, >= least] uint8 on GPU dev, whose rows may be
     parts of longer ones (a view of a buffer's columns)."""
-    import torch
-    if t.dtype is not torch.uint8:
-        raise TypeError(f"{what} is {t.dtype}, not {torch.uint8}")
+    if t.dtype is not _torch.uint8:
+        raise TypeError(f"{what} is {t.dtype}, not {_torch.uint8}")
     shape = t.shape
     if len(shape) != 2 or shape[0] != R or shape[1] < least:
         raise ValueError(f"{what} has shape {tuple(shape)}, not [{R}, {least}] or wider")
-    if not t.is_cuda:
-        raise ValueError(f"{what} is not on a GPU")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, not on GPU {dev}")
     pitch, step = t.stride()
     if R <= 1:  # the stride of an only row means nothing
         pitch = (shape[1] + 15) // 16 * 16
@@ -833,28 +863,29 @@ def llep_quantize_rows_mxfp4(x, q, scale, stream=None):
     """x [R, D] (bf16 or float32) to 4-bit rows: q [R, llep_mxfp4_row_bytes(D)] and scale [R,
     llep_mxfp4_scale_bytes(D)] uint8 (rows a multiple of 16 bytes apart)."""
     R, D = x.shape
-    code = _dtype_code(x)
-    _dense("x", x, (R, D), x.dtype)
+    code, _ = _type_code(x)
+    at = _arguments(stream, ("x", x, (R, D), x.dtype))
     q_bytes, s_bytes = _mxfp4_bytes(D)
-    q_pitch = _byte_rows("q", q, R, q_bytes)
-    s_pitch = _byte_rows("scale", scale, R, s_bytes)
-    _here(x, q, scale)
-    _check(lib().llep_quantize_rows_mxfp4(R, D, code, _ptr(x), _ptr(q), q_pitch, _ptr(scale),
-                                          s_pitch, _stream(stream)), "llep_quantize_rows_mxfp4")
+    dev = x.get_device()
+    q_pitch, s_pitch = _byte_rows("q", q, R, q_bytes, dev), _byte_rows("scale", scale, R, s_bytes, dev)
+    rc = lib().llep_quantize_rows_mxfp4(R, D, code, x.data_ptr(), q.data_ptr(), q_pitch,
+                                        scale.data_ptr(), s_pitch, at)
+    if rc:
+        _check(rc, "llep_quantize_rows_mxfp4")
 
 
 def llep_dequantize_rows_mxfp4(q, scale, out, stream=None):
     """out [R, D] (bf16 or float32) = what the 4-bit rows q, scale stand for."""
     R, D = out.shape
-    code = _dtype_code(out)
-    _dense("out", out, (R, D), out.dtype)
+    code, _ = _type_code(out)
+    at = _arguments(stream, ("out", out, (R, D), out.dtype))
     q_bytes, s_bytes = _mxfp4_bytes(D)
-    q_pitch = _byte_rows("q", q, R, q_bytes)
-    s_pitch = _byte_rows("scale", scale, R, s_bytes)
-    _here(q, scale, out)
-    _check(lib().llep_dequantize_rows_mxfp4(R, D, code, _ptr(q), q_pitch, _ptr(scale), s_pitch,
-                                            _ptr(out), _stream(stream)),
-           "llep_dequantize_rows_mxfp4")
+    dev = out.get_device()
+    q_pitch, s_pitch = _byte_rows("q", q, R, q_bytes, dev), _byte_rows("scale", scale, R, s_bytes, dev)
+    rc = lib().llep_dequantize_rows_mxfp4(R, D, code, q.data_ptr(), q_pitch, scale.data_ptr(),
+                                          s_pitch, out.data_ptr(), at)
+    if rc:
+        _check(rc, "llep_dequantize_rows_mxfp4")
 
 
 def llep_pack_matrix_mxfp4(w, scale, w_up=None, up_scale=None, K: int = None, stream=None):
@@ -890,18 +921,19 @@ def llep_pack_matrix_mxfp4(w, scale, w_up=None, up_scale=None, K: int = None, st
 def llep_mxfp4_matmul(x, x_scale, w_packed, out, K: int, stream=None):
     """out [M, N] (bf16 or float32) = x w^T: x, x_scale 4-bit rows of K values
     (llep_quantize_rows_mxfp4), w_packed one matrix of llep_pack_matrix_mxfp4."""
-    import torch
     M, N = out.shape
-    code = _dtype_code(out)
+    code, torch = _type_code(out)
     q_bytes, s_bytes = _mxfp4_bytes(K)
-    q_pitch = _byte_rows("x", x, M, q_bytes)
-    s_pitch = _byte_rows("x_scale", x_scale, M, s_bytes)
-    _dense("w_packed", w_packed, (1, (N + 15) // 16 * 16 * (q_bytes + s_bytes)), torch.uint8)
-    _dense("out", out, (M, N), out.dtype)
-    _here(x, x_scale, w_packed, out)
-    _check(lib().llep_mxfp4_matmul(M, N, K, _ptr(x), q_pitch, _ptr(x_scale), s_pitch,
-                                   _ptr(w_packed), code, _ptr(out), _stream(stream)),
-           "llep_mxfp4_matmul")
+    at = _arguments(stream, ("out", out, (M, N), out.dtype),
+                    ("w_packed", w_packed, (1, (N + 15) // 16 * 16 * (q_bytes + s_bytes)),
+                     torch.uint8))
+    dev = out.get_device()
+    q_pitch = _byte_rows("x", x, M, q_bytes, dev)
+    s_pitch = _byte_rows("x_scale", x_scale, M, s_bytes, dev)
+    rc = lib().llep_mxfp4_matmul(M, N, K, x.data_ptr(), q_pitch, x_scale.data_ptr(), s_pitch,
+                                 w_packed.data_ptr(), code, out.data_ptr(), at)
+    if rc:
+        _check(rc, "llep_mxfp4_matmul")
 
 
 def llep_grouped_ffn_mxfp4_workspace_bytes(params: llep_plan_params, F: int) -> int:
