@@ -140,7 +140,7 @@ __device__ __forceinline__ float unordered(uint32_t u) {
 }
 
 // A float64 with an index in its last 9 bits, the larger the lower the index: a
-// maximum of such numbers is one instruction (of 64-bit integers, five). An infinity
+// maximum of such numbers is one instruction (of 64-bit integers, three). An infinity
 // becomes the largest finite number.
 struct IndexedDouble {
   using V = double;
