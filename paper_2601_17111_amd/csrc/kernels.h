@@ -201,6 +201,7 @@ struct RouteArgs {
   int32_t *ids;
   float *gates;
   void *d_logits;
+  int32_t group_size, wide_log2;  // a group's experts, and (lists) its lanes: set by launch_route
 };
 hipError_t launch_route(const RouteArgs &a, bool backward, hipStream_t stream);
 

@@ -5,9 +5,9 @@
 // once, and neither scores nor keys go to memory. Up to 8 experts of a row are
 // found with sorted lists: every lane sorts its experts' keys eight (or four) at a
 // time and merges them into its best so far, then the lanes of a row merge theirs.
-// What the lists do not take (more than 8 experts, groups that are not whole lanes)
-// and what they cannot decide goes to rounds, a maximum over the row for each
-// expert (pick_exact).
+// What the lists do not take (more than 8 experts, more groups than lanes) and what
+// they cannot decide goes to rounds, a maximum over the row for each expert
+// (pick_exact).
 #include <math.h>
 
 #include <algorithm>
@@ -423,8 +423,19 @@ __global__ __launch_bounds__(kRouteThreads) void route_rounds_kernel(RouteArgs a
 }
 
 // ---------------------------------------------------------------------------
-// lists: lane t of a row's kLanes holds the experts t kPer .. + kPer - 1
+// lists: lane t of a row's kLanes holds kPer experts next to each other, of one group
+// (with groups, each has 2^wide_log2 lanes, the last of which may hold fewer)
 // ---------------------------------------------------------------------------
+
+struct LaneExperts {
+  int first, end;  // (first >= end: none)
+};
+template <int kPer>
+__device__ __forceinline__ LaneExperts lane_experts(const RouteArgs &a, int t) {
+  if (a.groups == 1) return {t * kPer, a.E};
+  const int g = t >> a.wide_log2, in = t & ((1 << a.wide_log2) - 1);
+  return {g * a.group_size + in * kPer, g < a.groups ? (g + 1) * a.group_size : 0};
+}
 
 template <typename V>
 __device__ __forceinline__ void order2(V &a, V &b) {
@@ -534,14 +545,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteArgs a)
     const int64_t row = row0 + lane_id() / kLanes;
     const L *logits = static_cast<const L *>(a.logits) + (row < a.T ? row : a.T - 1) * a.E;
     float l[kPer];
-    route_load_row<kPer>(logits, t * kPer, a.E, l);
+    const LaneExperts mine = lane_experts<kPer>(a, t);
+    route_load_row<kPer>(logits, mine.first, mine.end, l);
     V key[kPer], top[kTop];
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) key[j] = l[j] > -kInf ? Key::make(l[j], t * kPer + j) : Key::kNone;
+    for (int j = 0; j < kPer; ++j) key[j] = l[j] > -kInf ? Key::make(l[j], mine.first + j) : Key::kNone;
     lane_list(key, Key::kNone, top);
     if (kLanes == 16 && a.groups > 1) {
-      // groups of `wide` lanes: the best of each, then the groups before it
-      const int wide = a.E / a.groups / kPer;
+      // the best of each group, then the groups before it
+      const int wide = 1 << a.wide_log2;
       V own = top[0];
       auto fold = [&](V x) { own = larger(own, x); };
       if (wide > 1) fold(partner<1>(own));
@@ -634,10 +646,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
     const int64_t row = row0 + lane_id() / kLanes;
     const L *logits = static_cast<const L *>(a.logits) + (row < a.T ? row : a.T - 1) * a.E;
     float l[kPer], b[kPer];
-    route_load_row<kPer>(logits, t * kPer, a.E, l);
+    const LaneExperts mine = lane_experts<kPer>(a, t);
+    route_load_row<kPer>(logits, mine.first, mine.end, l);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) b[j] = 0.0f;
-    if (a.bias) route_load_row<kPer>(a.bias, t * kPer, a.E, b);
+    if (a.bias) route_load_row<kPer>(a.bias, mine.first, mine.end, b);
     float most = 0.0f, total = 0.0f;
     double s[kPer], scale = 1.0;
     if (softmax) {
@@ -665,13 +678,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const double k = fma(s[j], scale, double(b[j]));
-      key[j] = l[j] > -kInf && k > -__builtin_huge_val() ? Key::make(k, t * kPer + j) : kNone;
+      key[j] = l[j] > -kInf && k > -__builtin_huge_val() ? Key::make(k, mine.first + j) : kNone;
     }
     lane_list(key, kNone, top);
     bool doubt = false;
     if (a.groups > 1) {
-      // groups of `wide` lanes: the two best of each, then the groups before it
-      const int wide = a.E / a.groups / kPer;
+      // the two best of each group, then the groups before it
+      const int wide = 1 << a.wide_log2, own_group = t >> a.wide_log2;
       double one = top[0], two = top[1];
       auto fold = [&](double x, double y) {
         two = larger(larger(two, y), smaller(one, x));
@@ -683,13 +696,29 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
       if (kLanes == 64 && wide > 8) fold(partner<8>(one), partner<8>(two));
       double sum = Key::value(one);
       if (a.group_score == LLEP_GROUP_TOP2 && two != kNone) sum += Key::value(two);
-      const double own = one != kNone ? Key::make(sum, t / wide) : kNone;
+      const double own = one != kNone ? Key::make(sum, own_group) : kNone;
       int before = 0;
       for (int g = 0; g < a.groups; ++g) {
         const double other = __shfl(own, g * wide, kLanes);
         before += other > own;
         // (whether the two are on both sides of the border is left to pick_exact)
-        if (g != t / wide && other != kNone && own != kNone) doubt |= near(other, own);
+        if (g != own_group && other != kNone && own != kNone) doubt |= near(other, own);
+      }
+      // Of 8192 rows of bfloat16 logits without a bias hundreds have two groups whose two
+      // best are equal: their order is known (8192 x 160 30 -> 12 us).
+      if (__any(doubt)) {
+        const bool both = a.group_score == LLEP_GROUP_TOP2 && two != kNone;
+        const int e = one != kNone ? Key::index(one) : 0, f = both ? Key::index(two) : 0;
+        const float le = route_load(logits + e), lf = both ? route_load(logits + f) : -kInf;
+        const float be = a.bias ? a.bias[e] : 0.0f, bf = a.bias && both ? a.bias[f] : 0.0f;
+        doubt = false;
+        for (int g = 0; g < a.groups; ++g) {
+          const double other = __shfl(own, g * wide, kLanes);
+          const bool equal =
+              __shfl(le, g * wide, kLanes) == le && __shfl(lf, g * wide, kLanes) == lf &&
+              __shfl(be, g * wide, kLanes) == be && __shfl(bf, g * wide, kLanes) == bf;
+          if (g != own_group && other != kNone && own != kNone) doubt |= near(other, own) && !equal;
+        }
       }
       if (before >= a.top_groups) {
 #pragma unroll
@@ -892,6 +921,27 @@ hipError_t lists_per(const RouteArgs &a, int per, hipStream_t stream) {
   }
 }
 
+template <typename L, int kLanes, bool kSum>
+hipError_t lists_top(const RouteArgs &a, int per, hipStream_t stream) {
+  return a.K <= 4 ? lists_per<L, kLanes, 4, kSum>(a, per, stream)
+                  : lists_per<L, kLanes, 8, kSum>(a, per, stream);
+}
+// Experts of a lane (and a group's lanes, into `a`), 0: the groups do not fit.
+static int list_shape(RouteArgs &a, int lanes) {
+  const int least = lanes == 64 ? 2 : 8, most = lanes == 64 ? 16 : 8;  // lanes of a group
+  int held = lanes;
+  if (a.groups > 1) {
+    if (a.groups > lanes) return 0;
+    while (a.wide_log2 < 6 && (2 << a.wide_log2) * a.groups <= lanes && (2 << a.wide_log2) <= most &&
+           (least << a.wide_log2) < a.group_size)
+      ++a.wide_log2;
+    held = 1 << a.wide_log2;
+  }
+  int per = least;
+  while (per < 4 * least && per * held < a.group_size) per *= 2;
+  return per * held >= a.group_size ? per : 0;
+}
+
 template <typename L>
 hipError_t route_t(const RouteArgs &a, bool backward, hipStream_t stream) {
   static_assert(LLEP_MAX_EXPERTS == 512 && LLEP_MAX_ROUTE_TOPK == 64, "a row fits a wavefront");
@@ -902,26 +952,19 @@ hipError_t route_t(const RouteArgs &a, bool backward, hipStream_t stream) {
   // 4096 x 32 3.4 / 3.0. (More than 8 experts of 128, 64 / 16: 2048 rows 4.8 / 5.1, 4096
   // 6.5 / 5.3; the gradient of 8 of 128: 4096 3.4 / 3.6, 8192 4.2 / 3.7.)
   if (!backward && a.K <= 8) {
-    const int lanes = sum ? (a.T <= 1024 ? 64 : 16)
-                          : ((a.T < 12288 && a.E > 32) || a.E > 128 || a.groups > 1 ? 16 : 4);
-    const int least = lanes == 64 ? 2 : 8;
-    int per = least;  // experts of a lane
-    while (per < 4 * least && per * lanes < a.E) per *= 2;
-    // groups: 1, 2, 4 or 8 whole lanes (16 of 64)
-    const int size = a.E / a.groups, wide = size / per;
-    if (a.groups == 1 ||
-        (size % per == 0 && wide <= (lanes == 64 ? 16 : 8) && (wide & (wide - 1)) == 0)) {
-      if (sum && lanes == 64)
-        return a.K <= 4 ? lists_per<L, 64, 4, true>(a, per, stream)
-                        : lists_per<L, 64, 8, true>(a, per, stream);
-      if (sum)
-        return a.K <= 4 ? lists_per<L, 16, 4, true>(a, per, stream)
-                        : lists_per<L, 16, 8, true>(a, per, stream);
-      if (lanes == 16)
-        return a.K <= 4 ? lists_per<L, 16, 4, false>(a, per, stream)
-                        : lists_per<L, 16, 8, false>(a, per, stream);
-      return a.K <= 4 ? lists_per<L, 4, 4, false>(a, per, stream)
-                      : lists_per<L, 4, 8, false>(a, per, stream);
+    const bool few = sum && a.T <= 1024;
+    const int lanes = few                                                         ? 64
+                      : sum || (a.T < 12288 && a.E > 32) || a.E > 128 || a.groups > 1 ? 16
+                                                                                      : 4;
+    // (64 lanes hold 8 experts each at most, which few large groups do not fit)
+    for (int n : {lanes, few ? 16 : lanes}) {
+      RouteArgs b = a;
+      const int per = list_shape(b, n);
+      if (per == 0) continue;
+      if (n == 64)
+        return lists_top<L, 64, true>(b, per, stream);
+      if (n == 4) return lists_top<L, 4, false>(b, per, stream);
+      return sum ? lists_top<L, 16, true>(b, per, stream) : lists_top<L, 16, false>(b, per, stream);
     }
   }
   if (a.T <= (backward ? 4096 : 2048) || a.K > 16) {
@@ -939,8 +982,11 @@ hipError_t route_t(const RouteArgs &a, bool backward, hipStream_t stream) {
 
 hipError_t launch_route(const RouteArgs &a, bool backward, hipStream_t stream) {
   if (a.T == 0) return hipSuccess;
-  return a.dtype == LLEP_BF16 ? route_t<uint16_t>(a, backward, stream)
-                              : route_t<float>(a, backward, stream);
+  RouteArgs b = a;
+  b.group_size = a.E / a.groups;
+  b.wide_log2 = 0;
+  return a.dtype == LLEP_BF16 ? route_t<uint16_t>(b, backward, stream)
+                              : route_t<float>(b, backward, stream);
 }
 
 }  // namespace llep

@@ -97,6 +97,44 @@ def test_groups(dev, E, G, top, K, by, bias):
            top_groups=top, group_score=by)
 
 
+@pytest.mark.parametrize("T", [70, 1300])
+@pytest.mark.parametrize("E,G,top,K", [(160, 8, 3, 6), (72, 8, 3, 4), (480, 8, 3, 8), (500, 5, 2, 8),
+                                       (510, 2, 1, 8), (33, 3, 2, 3), (48, 16, 5, 8), (51, 17, 6, 4),
+                                       (510, 51, 20, 8), (64, 64, 9, 8), (60, 20, 7, 7), (511, 7, 3, 8)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_groups_of_any_size(dev, T, E, G, top, K, dtype):
+    """Groups that are not whole lanes, with equal logits and equal groups (bfloat16) among them."""
+    import torch
+    l, b = _logits(E + G, T, E, masked=0.05)
+    at = np.unique(np.concatenate([np.arange(0, T, max(1, T // 60)), [T - 1]]))
+    for bias in (None, b, torch.zeros(E)):
+        for by in ("max", "top2"):
+            how = dict(score="sigmoid" if K % 2 else "softmax", groups=G, top_groups=top, group_score=by)
+            _, x, _, ids, gates = _route(dev, l, K, bias, getattr(torch, dtype), **how)
+            want_ids, want = oracle.route(x.float().cpu().numpy()[at], K,
+                                          bias=None if bias is None else bias.numpy(), **how)
+            assert np.array_equal(ids.cpu().numpy()[at], want_ids)
+            near = 64 * U * np.abs(want) + 2.0 ** -148
+            assert np.all(np.abs(gates.double().cpu().numpy()[at] - want) <= near)
+
+
+def test_groups_of_equal_logits(dev):
+    """Few different logits: most groups tie, in one score or in both."""
+    import torch
+    g = torch.Generator().manual_seed(7)
+    for T in (60, 1100):
+        l = torch.randint(-1, 2, (T, 64), generator=g).float()
+        b = torch.randint(0, 2, (64,), generator=g).float() * 0.5
+        for bias in (None, b, torch.zeros(64)):
+            for score in ("softmax", "sigmoid"):
+                for K in (4, 8):
+                    how = dict(score=score, groups=8, top_groups=3, group_score="top2")
+                    _, x, _, ids, _ = _route(dev, l, K, bias, torch.bfloat16, **how)
+                    want, _ = oracle.route(l.numpy()[-60:], K, bias=None if bias is None else bias.numpy(),
+                                           **how)
+                    assert np.array_equal(ids.cpu().numpy()[-60:], want)
+
+
 @pytest.mark.parametrize("T,E,K", [(20000, 128, 8), (20000, 40, 4), (17000, 64, 5), (5000, 256, 8),
                                    (4500, 33, 12)])
 def test_long_batches(dev, T, E, K):
