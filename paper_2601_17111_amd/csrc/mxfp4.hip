@@ -61,13 +61,13 @@ struct MxRowItems {
   }
 };
 
-// kPast: values of more than the 256 MB cache behind the L2s are loaded past it, and
-// stored past it by the kernel below (92160 x 2880 132 -> 119 us and 136 -> 101), 4-bit
-// rows only where they are as many themselves (2: 200000 x 2880 and back 580 -> 560, but
-// 92160 x 2880 220 -> 248, which finds its 4-bit rows in the cache). With less, the call
-// that reads the results takes longer for it than these save (8192 x 2880 and 2880 x
-// 2880 weights 63 -> 71; values back and a read of them 26.7 -> 28.4).
-template <typename T, bool kOdd, int kPast>
+// kPast: values of more than the 256 MB cache behind the L2s, which loads and stores go
+// past (92160 x 2880 132 -> 119 us, and 136 -> 101 for the values back; both, on buffers
+// in turn, 260 with the 4-bit rows through the cache, 249 past it, though on the same
+// buffers again and again 221 and 248). With less, the call that reads the results takes
+// longer for it than these save (8192 x 2880 and 2880 x 2880 weights 63 -> 71; values
+// back and a read of them 26.7 -> 28.4).
+template <typename T, bool kOdd, bool kPast>
 __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRowsArgs a) {
   const int lane = lane_id();
   const int q_bytes = (a.D + kSliceK - 1) / kSliceK * 64;
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRows
       const T *p = static_cast<const T *>(a.x) + row * a.D + c;
       if constexpr (kOdd)
         in.load_any(p, a.D - c);
-      else if constexpr (kPast > 0)
+      else if constexpr (kPast)
 #pragma unroll
         for (int j = 0; j < RawVec<T, 8>::kWords; ++j)
           in.w[j] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(p) + j);
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kMxRowWaves * kWave) void mx_quantize_kernel(MxRows
       const uint32_t v = mx_pack4(in[0], in[1], in[2], in[3], step) |
                          (mx_pack4(in[4], in[5], in[6], in[7], step) << 16);
       uint32_t *to = reinterpret_cast<uint32_t *>(a.q + row * a.q_pitch + c / 2);
-      if constexpr (kPast == 2)
+      if constexpr (kPast)
         __builtin_nontemporal_store(v, to);
       else
         *to = v;
@@ -177,19 +177,17 @@ hipError_t launch_quantize_mxfp4(int64_t R, int32_t D, llep_dtype dtype, const v
   const bool whole = D % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
   const dim3 grid = mx_rows_grid(a), threads(kMxRowWaves * kWave);
   if (dtype == LLEP_BF16) {
-    if (whole && mx_past_cache(R * mx_row_bytes(D)))
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, 2>), grid, threads, 0, stream, a);
-    else if (whole && mx_past_cache(R * D * 2))
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, 1>), grid, threads, 0, stream, a);
+    if (whole && mx_past_cache(R * D * 2))
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, true>), grid, threads, 0, stream, a);
     else if (whole)
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, 0>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, false, false>), grid, threads, 0, stream, a);
     else
-      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, true, 0>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<uint16_t, true, false>), grid, threads, 0, stream, a);
   } else {
     if (whole)
-      hipLaunchKernelGGL((mx_quantize_kernel<float, false, 0>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<float, false, false>), grid, threads, 0, stream, a);
     else
-      hipLaunchKernelGGL((mx_quantize_kernel<float, true, 0>), grid, threads, 0, stream, a);
+      hipLaunchKernelGGL((mx_quantize_kernel<float, true, false>), grid, threads, 0, stream, a);
   }
   return hipGetLastError();
 }
