@@ -169,6 +169,28 @@ def test_layer(dev, T):
             assert torch.equal(r, r2) and torch.equal(h, h2)
 
 
+@pytest.mark.parametrize("T", [6, 90, 1500])
+def test_tokens_that_are_not_finite(dev, T):
+    """A token with a NaN or an infinity is NaN, the others are as without it; in the stream and in
+    tiles."""
+    import torch
+    from paper_2601_17111_amd.layer import LLEPLayer
+    K, E, P, D, F = 2, 4, 2, 704, 640
+    g = np.random.default_rng(T)
+    experts, _ = _experts(g, dev, E, D, F)
+    ids = torch.from_numpy(g.integers(0, E, (T, K)).astype(np.int32)).to(dev)
+    gates = torch.from_numpy(g.uniform(0.1, 1, (T, K)).astype(np.float32)).to(dev)
+    x = torch.from_numpy(g.normal(size=(T, D))).to(dev).bfloat16()
+    layer = LLEPLayer(T, K, E, P, D, F, -(-T * K * 11 // (10 * P)), torch.bfloat16, dev)
+    want = layer.forward_mxfp4(ids, gates, x, experts).clone()
+    bad = x.clone()
+    bad[1, 3], bad[T - 1, D - 1], bad[T // 2, 40] = math.nan, math.inf, -math.inf
+    got = layer.forward_mxfp4(ids, gates, bad, experts)
+    rows = torch.zeros(T, dtype=torch.bool, device=dev)
+    rows[[1, T // 2, T - 1]] = True
+    assert bool(torch.isnan(got[rows]).all()) and torch.equal(got[~rows], want[~rows])
+
+
 def test_experts_from_weights(dev):
     """from_weights packs the 4-bit rows of the transposed weights."""
     import torch
