@@ -351,6 +351,24 @@ def test_backward_of_repeated_and_bad_ids(dev, score, renormalize):
     _check_backward(dev, l, ids, 3, torch.float32, score, renormalize, 1.0)
 
 
+@pytest.mark.parametrize("T,E,K", [(37, 40, 3), (5003, 128, 8), (4099, 300, 16)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_backward_in_place(dev, T, E, K, dtype):
+    """The gradient may take the place of the logits."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    l, _ = _logits(E, T, E, masked=0.05)
+    d = torch.randn(T, K, device=dev)
+    for score in ("softmax", "sigmoid"):
+        for renormalize in (True, False):
+            p, x, _, ids, gates = _route(dev, l, K, dtype=getattr(torch, dtype), score=score,
+                                         renormalize=renormalize)
+            want = torch.empty_like(x)
+            B.llep_route_backward(p, x, ids, gates, d, want)
+            B.llep_route_backward(p, x, ids, gates, d, x)
+            assert torch.equal(x, want)
+
+
 def test_backward_leaves_gates_of_masked_pairs_out(dev):
     """What stands in the gates and gradients of pairs without an expert does not matter."""
     import torch
