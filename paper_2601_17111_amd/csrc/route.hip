@@ -604,14 +604,16 @@ __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteArgs a)
 }
 
 // Keys that are sums of scores, float64, cut to 43 bits of fraction with the index
-// below them (IndexedDouble). Keys (and groups' scores) nearer to each other than
-// kDoubt, of 1 (a score is at most 1, and a bias rounds the sum in units of itself)
-// or of the larger, may be in another order than uncut ones, or computed in another
-// order of the softmax's sum: where that is so among the chosen, between the last of
-// them and the next, or between a group and another, all rows of the wavefront go to
-// pick_exact, unless equal logits and biases say that keys are equal. With random
-// logits hardly any do (with keys in float32 ten of 8192 rows of 256 experts did, and
-// the launch, of 24 us, was as long as theirs).
+// below them (IndexedDouble). Keys nearer to each other than kDoubt, of 1 (a score is at
+// most 1, and a bias rounds the sum in units of itself) or of the larger, may be in
+// another order than uncut ones, or computed in another order of the softmax's sum. The
+// sum of a group's two best is off by up to 2^-42 of the larger of them, cut again by as
+// much, however small the sum is (a bias of +64 and one of -64): groups are told apart
+// beyond 2 kDoubt of the largest key that went into either. Where keys are nearer among
+// the chosen, between the last of them and the next, or between two groups, all rows of
+// the wavefront go to pick_exact, unless equal logits and biases say that keys are equal.
+// With random logits hardly any do (with keys in float32 ten of 8192 rows of 256 experts
+// did, and the launch, of 24 us, was as long as theirs).
 constexpr double kDoubt = 0x1p-40;
 
 // 1 / d for 1 <= d, in float64 up to a rounding or two (of an infinity: not 0, but
@@ -694,30 +696,34 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
       if (wide > 2) fold(partner<2>(one), partner<2>(two));
       if (wide > 4) fold(partner<4>(one), partner<4>(two));
       if (kLanes == 64 && wide > 8) fold(partner<8>(one), partner<8>(two));
-      double sum = Key::value(one);
-      if (a.group_score == LLEP_GROUP_TOP2 && two != kNone) sum += Key::value(two);
+      const bool both = a.group_score == LLEP_GROUP_TOP2 && two != kNone;
+      double sum = Key::value(one), size = one != kNone ? fabs(sum) : 0.0;
+      if (both) sum += Key::value(two), size = fmax(size, fabs(Key::value(two)));
       const double own = one != kNone ? Key::make(sum, own_group) : kNone;
+      const double limit = 2.0 * kDoubt * fmax(unit, row_max<kLanes>(size));
       int before = 0;
       for (int g = 0; g < a.groups; ++g) {
         const double other = __shfl(own, g * wide, kLanes);
         before += other > own;
         // (whether the two are on both sides of the border is left to pick_exact)
-        if (g != own_group && other != kNone && own != kNone) doubt |= near(other, own);
+        if (g != own_group && other != kNone && own != kNone)
+          doubt |= fabs(Key::value(other) - Key::value(own)) <= limit;
       }
-      // Of 8192 rows of bfloat16 logits without a bias hundreds have two groups whose two
-      // best are equal: their order is known (8192 x 160 30 -> 12 us).
+      // Pair by pair. Of 8192 rows of bfloat16 logits without a bias hundreds have two
+      // groups whose two best are equal: their order is known (8192 x 160 30 -> 12 us).
       if (__any(doubt)) {
-        const bool both = a.group_score == LLEP_GROUP_TOP2 && two != kNone;
         const int e = one != kNone ? Key::index(one) : 0, f = both ? Key::index(two) : 0;
         const float le = route_load(logits + e), lf = both ? route_load(logits + f) : -kInf;
         const float be = a.bias ? a.bias[e] : 0.0f, bf = a.bias && both ? a.bias[f] : 0.0f;
         doubt = false;
         for (int g = 0; g < a.groups; ++g) {
           const double other = __shfl(own, g * wide, kLanes);
+          const double most_key = fmax(unit, fmax(size, __shfl(size, g * wide, kLanes)));
           const bool equal =
               __shfl(le, g * wide, kLanes) == le && __shfl(lf, g * wide, kLanes) == lf &&
               __shfl(be, g * wide, kLanes) == be && __shfl(bf, g * wide, kLanes) == bf;
-          if (g != own_group && other != kNone && own != kNone) doubt |= near(other, own) && !equal;
+          if (g != own_group && other != kNone && own != kNone)
+            doubt |= fabs(Key::value(other) - Key::value(own)) <= 2.0 * kDoubt * most_key && !equal;
         }
       }
       if (before >= a.top_groups) {

@@ -1,0 +1,99 @@
+"""The choice of experts where keys lie closer than the kernels' sorted keys tell
+apart: group sums whose two keys cancel, keys hidden behind equal ones, scores that
+are nothing next to each other; against the oracle's float64 keys, ids exactly, in
+few and in many rows (64 and 16 lanes a row).
+
+Ids are compared exactly although a score of the kernel and one of the oracle may
+differ by a step or two of float64: the logits here are such that no key lies within
+two steps of a score of a border between two roundings (test_logits_are_off_the_borders
+computes that in 60 digits), or such that the scores' differences are far above them."""
+
+from decimal import Decimal, getcontext
+
+import numpy as np
+import pytest
+
+import oracle
+from gpu_util import device
+
+gpu = pytest.mark.gpu
+
+# sigmoids of these have no key within two steps under the biases of CANCEL
+FEW = (-1.5, -1.0, 0.0, 1.0, 1.5)
+CANCEL = (16.0, 64.0, 1000.0)
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return device()
+
+
+def _same_ids(dev, l, K, bias=None, rows=None, dtype="float32", **how):
+    """llep_route's ids of logits [T, E] against the oracle's (of `rows` of them)."""
+    import torch
+    from paper_2601_17111_amd import binding as B
+    x = torch.from_numpy(np.ascontiguousarray(l, dtype=np.float32)).to(getattr(torch, dtype)).to(dev)
+    T, E = x.shape
+    b = None if bias is None else torch.from_numpy(np.asarray(bias, dtype=np.float32)).to(dev)
+    ids = torch.full((T, K), 77, dtype=torch.int32, device=dev)
+    gates = torch.empty((T, K), device=dev)
+    B.llep_route(B.make_route(T, K, E, **how), x, b, ids, gates)
+    rows = np.arange(T) if rows is None else rows
+    want, _ = oracle.route(x.float().cpu().numpy()[rows], K, bias=None if b is None else b.cpu().numpy(),
+                           **how)
+    got = ids.cpu().numpy()[rows]
+    bad = np.nonzero((got != want).any(1))[0]
+    assert len(bad) == 0, (rows[bad[:3]], got[bad[:3]], want[bad[:3]], len(bad))
+
+
+def test_logits_are_off_the_borders():
+    getcontext().prec = 60
+    for l in FEW:
+        s = 1 / (1 + (-Decimal(l)).exp())
+        step = Decimal(float(np.spacing(float(s))))
+        for bias in CANCEL:
+            for b in (bias, -bias):
+                key = s + Decimal(b)
+                k = float(key)
+                half = Decimal(float(np.spacing(abs(k)))) / 2
+                border = min(abs(key - Decimal(k) - half), abs(key - Decimal(k) + half))
+                assert border > 2 * step, (l, b)
+
+
+@gpu
+def test_group_sums_that_cancel(dev):
+    """Two keys of 64 and -65 whose sum decides: its cut is that of the keys."""
+    l = np.array([[0.0, 4e-13, 4 * 2.0 ** -37 - 4e-13, 0.0]])
+    how = dict(score="sigmoid", groups=2, top_groups=1, group_score="top2")
+    for T in (1, 60, 1100):
+        _same_ids(dev, np.repeat(l, T, 0), 2, [64.0, -65.0, 64.0, -65.0], **how)
+
+
+@gpu
+@pytest.mark.parametrize("T", [700, 1100])
+@pytest.mark.parametrize("E,G,top", [(32, 16, 5), (32, 16, 8), (64, 8, 3), (256, 8, 4)])
+@pytest.mark.parametrize("size", CANCEL)
+def test_groups_of_large_biases_of_both_signs(dev, T, E, G, top, size):
+    """Few different logits, whose sums differ by the roundings of the keys alone."""
+    g = np.random.default_rng(int(size) + E + top)
+    rows = np.unique(np.concatenate([np.arange(0, T, 2 if E < 100 else 12), [T - 1]]))
+    for _ in range(2):
+        _same_ids(dev, g.choice(FEW, (T, E)), 4, g.choice([-size, size], E), rows, score="sigmoid",
+                  groups=G, top_groups=top, group_score="top2")
+
+
+@gpu
+@pytest.mark.parametrize("T", [700, 1100])
+@pytest.mark.parametrize("size,around", [(64.0, -22.0), (1e3, -22.0), (1e11, 0.0), (1e12, 0.0)])
+def test_groups_whose_two_best_cancel(dev, T, size, around):
+    """Every group's best expert is raised by as much as its second is lowered."""
+    E, G = 64, 8
+    g = np.random.default_rng(int(size) % 97)
+    rows = np.arange(0, T, 2)
+    for _ in range(2):
+        b = np.full(E, -3 * size)
+        for e in range(0, E, E // G):
+            at = e + g.permutation(E // G)[:2]
+            b[at] = size, -size
+        _same_ids(dev, around + g.normal(size=(T, E)), 2, b, rows, score="sigmoid", groups=G, top_groups=4,
+                  group_score="top2")
