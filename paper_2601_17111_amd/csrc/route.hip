@@ -610,7 +610,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteArgs a)
 // sum of a group's two best is off by up to 2^-42 of the larger of them, cut again by as
 // much, however small the sum is (a bias of +64 and one of -64): groups are told apart
 // beyond 2 kDoubt of the largest key that went into either. Where keys are nearer among
-// the chosen, between the last of them and the next, or between two groups, all rows of
+// the chosen, between the last of them and any other, or between two groups, all rows of
 // the wavefront go to pick_exact, unless equal logits and biases say that keys are equal.
 // With random logits hardly any do (with keys in float32 ten of 8192 rows of 256 experts
 // did, and the launch, of 24 us, was as long as theirs).
@@ -639,6 +639,21 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
   auto near = [&](double x, double y) {  // neither of them none
     const double u = Key::value(x), v = Key::value(y);
     return fabs(u - v) <= kDoubt * fmax(unit, fmax(fabs(u), fabs(v)));
+  };
+  // whether one of the lane's keys below `last` is near it without being equal
+  auto another_near = [&](const double (&key)[kPer], double last, const L *logits) {
+    if (last == kNone) return false;
+    const int e = Key::index(last);
+    const float l = route_load(logits + e), b = a.bias ? a.bias[e] : 0.0f;
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (key[j] < last && key[j] != kNone && near(key[j], last)) {
+        const int f = Key::index(key[j]);
+        found |= route_load(logits + f) != l || (a.bias && a.bias[f] != b);
+      }
+    }
+    return found;
   };
   // every lane of a wavefront takes part in the reductions, also past the end
   for (int64_t row0 = first_row<kRows, kLanes>(); row0 < a.T; row0 += step) {
@@ -734,22 +749,25 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
       }
     }
     row_list<kLanes>(top);
-    // the lane's one of the chosen, and the next one behind it
+    // the lane's one of the chosen, and the next of them
     const double v = list_slot<kTop, 1>(top, t, 0, a.K, kNone);
-    double w = list_slot<kTop, 1>(top, t + 1, 0, a.K, kNone);
-    double last = top[0], next = kNone;
-#pragma unroll
-    for (int k = 1; k < kTop; ++k)
-      if (k < a.K) last = top[k];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) next = larger(next, key[j] < last ? key[j] : kNone);
-    next = row_max<kLanes>(next);
-    if (t == a.K - 1) w = next;
+    const double w = list_slot<kTop, 1>(top, t + 1, 0, a.K, kNone);
     if (w != kNone && near(v, w)) {
       const int e = Key::index(v), f = Key::index(w);
       doubt |= Key::value(v) != Key::value(w) || route_load(logits + e) != route_load(logits + f) ||
                (a.bias && a.bias[e] != a.bias[f]);
     }
+    // the last of them, and what is as near (which may be equal to it, or hidden behind
+    // one that is)
+    double last = top[0];
+#pragma unroll
+    for (int k = 1; k < kTop; ++k)
+      if (k < a.K) last = top[k];
+    const double low = Key::value(last) - kDoubt * fmax(unit, fabs(last));
+    bool border = false;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) border |= key[j] < last && key[j] >= low;
+    if (__any(border)) doubt |= another_near(key, last, logits);
     int id[1] = {v != kNone ? Key::index(v) : -1};
     if (__any(doubt)) {
       id[0] = pick_exact<L, kPer, kLanes, false, true>(

@@ -97,3 +97,34 @@ def test_groups_whose_two_best_cancel(dev, T, size, around):
             b[at] = size, -size
         _same_ids(dev, around + g.normal(size=(T, E)), 2, b, rows, score="sigmoid", groups=G, top_groups=4,
                   group_score="top2")
+
+
+# saturated sigmoids: 1 - s is 9.4e-14 for 30, 7.7e-14 for 30.2, less apart than a cut key's
+# step of 5.7e-14 and far more than a step of float64 (1.1e-16)
+HIDDEN = [
+    # the last of the chosen, one that is equal to it, and behind both a larger one
+    (1, [30, 30, 30.2, 0, 1, 2, 3, 4], None),
+    (1, [0, 30, 1, 30, 30, 2, 30, 30.25], None),
+    (3, [3, 2, 30, 1, 30, 0, 0.5, 30.2], [1, 1, 0, 0, 0, 0, 0, 0]),
+    (4, [3, 2, 30, 1, 30, 30.2, 30, 30.2], [1, 1, 0, 0, 0, 0, 0, 0]),
+    # the same, below zero
+    (2, [1, 30, 30, 30.2, 0, 0, 0, 0], [4, -3, -3, -3, -9, -9, -9, -9]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("K,row,bias", HIDDEN)
+def test_a_key_hidden_behind_an_equal_one(dev, K, row, bias):
+    """Among rows of which the same is true, in whatever order of the experts, and others."""
+    E = len(row)
+    g = np.random.default_rng(K)
+    for T in (1, 60, 1100):
+        for wide in (E, 40, 200):
+            l = np.full((T, wide), -4.0) + 0.25 * (np.arange(wide) % 7)
+            l[:, wide - E:] = row
+            if T > 1:
+                l[1::3] += g.normal(size=l[1::3].shape)
+            b = np.zeros(wide) if bias is None else np.r_[np.full(wide - E, -9.0), bias]
+            rows = np.unique(np.r_[np.arange(0, T, 17), T - 1])
+            for dtype in ("float32", "bfloat16"):
+                _same_ids(dev, l, K, b, rows, dtype, score="sigmoid")
