@@ -725,18 +725,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
           doubt |= fabs(Key::value(other) - Key::value(own)) <= limit;
       }
       // Pair by pair. Of 8192 rows of bfloat16 logits without a bias hundreds have two
-      // groups whose two best are equal: their order is known (8192 x 160 30 -> 12 us).
+      // groups whose two best are equal: their order is known (8192 x 160 30 -> 12 us), if
+      // no other key of theirs is as near.
       if (__any(doubt)) {
         const int e = one != kNone ? Key::index(one) : 0, f = both ? Key::index(two) : 0;
         const float le = route_load(logits + e), lf = both ? route_load(logits + f) : -kInf;
         const float be = a.bias ? a.bias[e] : 0.0f, bf = a.bias && both ? a.bias[f] : 0.0f;
+        const uint64_t others = __ballot(another_near(key, both ? two : one, logits));
+        const int sure = ((others >> (lane_id() & -wide)) & ((1u << wide) - 1)) == 0;
         doubt = false;
         for (int g = 0; g < a.groups; ++g) {
           const double other = __shfl(own, g * wide, kLanes);
           const double most_key = fmax(unit, fmax(size, __shfl(size, g * wide, kLanes)));
           const bool equal =
               __shfl(le, g * wide, kLanes) == le && __shfl(lf, g * wide, kLanes) == lf &&
-              __shfl(be, g * wide, kLanes) == be && __shfl(bf, g * wide, kLanes) == bf;
+              __shfl(be, g * wide, kLanes) == be && __shfl(bf, g * wide, kLanes) == bf &&
+              (__shfl(sure, g * wide, kLanes) & sure);
           if (g != own_group && other != kNone && own != kNone)
             doubt |= fabs(Key::value(other) - Key::value(own)) <= 2.0 * kDoubt * most_key && !equal;
         }

@@ -128,3 +128,28 @@ def test_a_key_hidden_behind_an_equal_one(dev, K, row, bias):
             rows = np.unique(np.r_[np.arange(0, T, 17), T - 1])
             for dtype in ("float32", "bfloat16"):
                 _same_ids(dev, l, K, b, rows, dtype, score="sigmoid")
+
+
+# groups whose best ones are equal, and of one of them another that is larger by less than a cut key
+# tells (30 against 30.2; 26 against 26 + 2^-7: 1 - s is 5.1e-12, its difference 4.0e-14)
+HIDDEN_GROUPS = [
+    ("max", 2, [30, 20, 0, 0, 30, 30.2, 0, 0], True, 1),
+    ("max", 2, [30, 1, 30, 2, 30, 30, 30.2, 20], True, 1),
+    ("top2", 2, [30, 26, 0, 1, 30, 26, 26 + 2.0 ** -7, 1], False, 1),
+    ("top2", 2, [30, 26, 0, 1, 30, 26, 26 + 2.0 ** -7, 1], True, 1),
+    ("top2", 2, [30, 26, 0, 1, 0, 1, 2, 3, 26, 30, 1, 26 + 2.0 ** -7, 4, 3, 2, 1], False, 1),
+]
+
+
+@gpu
+@pytest.mark.parametrize("by,K,row,bias,top", HIDDEN_GROUPS)
+def test_a_group_that_is_larger_by_a_hidden_key(dev, by, K, row, bias, top):
+    E, size = len(row), 4
+    for T in (1, 60, 1100):
+        for groups in (E // size, 8, 16):
+            l = np.full((T, groups * size), -4.0) + 0.25 * (np.arange(groups * size) % 7)
+            l[:, groups * size - E:] = row
+            for dtype in ("float32", "bfloat16"):
+                _same_ids(dev, l, K, np.zeros(groups * size) if bias else None, None if T < 100 else
+                          np.arange(0, T, 37), dtype, score="sigmoid", groups=groups, top_groups=top,
+                          group_score=by)
