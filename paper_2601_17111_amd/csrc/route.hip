@@ -635,7 +635,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_sums_kernel(RouteArgs a) 
   const float kInf = __builtin_huge_valf();
   const int64_t step = int64_t(gridDim.x) * kRows;
   const bool softmax = a.score == LLEP_SCORE_SOFTMAX;
-  const double unit = a.bias ? 1.0 : 0.0;
+  // (without a bias: sigmoids below 1e-300, which reciprocal() does not tell apart)
+  const double unit = a.bias ? 1.0 : 0x1p-900;
   auto near = [&](double x, double y) {  // neither of them none
     const double u = Key::value(x), v = Key::value(y);
     return fabs(u - v) <= kDoubt * fmax(unit, fmax(fabs(u), fabs(v)));

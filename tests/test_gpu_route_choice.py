@@ -153,3 +153,16 @@ def test_a_group_that_is_larger_by_a_hidden_key(dev, by, K, row, bias, top):
                 _same_ids(dev, l, K, np.zeros(groups * size) if bias else None, None if T < 100 else
                           np.arange(0, T, 37), dtype, score="sigmoid", groups=groups, top_groups=top,
                           group_score=by)
+
+
+@gpu
+@pytest.mark.parametrize("low", [-1e3, -1e9, float(np.finfo(np.float32).min)])
+def test_groups_of_nothing_but_scores_of_zero(dev, low):
+    """Masks by a low finite value: groups of such experts are equal, also where -infinity leaves one
+    of them a single expert."""
+    inf = np.inf
+    for T in (1, 60, 1100):
+        for row in ([1.0, 2.0, low, -inf, low, low], [low, -inf, -inf, low, 1.0, 2.0],
+                    [low, -inf, -inf, low, low, low]):
+            _same_ids(dev, np.repeat([row], T, 0), 4, score="sigmoid", groups=3, top_groups=2,
+                      group_score="top2")
