@@ -852,10 +852,12 @@ def _byte_rows(what: str, t, R: int, least: int, dev: int) -> int:
     if t.get_device() != dev:
         raise ValueError(f"{what} is on {t.device}, not on GPU {dev}")
     pitch, step = t.stride()
-    if R <= 1:  # the stride of an only row means nothing
-        pitch = (shape[1] + 15) // 16 * 16
-    if step != 1 or pitch < shape[1]:
+    if step != 1 or (R > 1 and pitch < shape[1]):
         raise ValueError(f"{what} is not made of rows of bytes")
+    if R <= 1:  # the stride of an only row means nothing
+        return least
+    if pitch >= 1 << 31:
+        raise ValueError(f"{what} has rows {pitch} bytes apart, 2^31 or more")
     return pitch
 
 
@@ -899,6 +901,8 @@ def llep_pack_matrix_mxfp4(w, scale, w_up=None, up_scale=None, K: int = None, st
     E, N, w_bytes = (1, *w.shape) if w.dim() == 2 else w.shape
     if K is None:
         K = 2 * w_bytes
+    if max(E, N, w_bytes, scale.shape[-1], K) >= 1 << 31:
+        raise ValueError("weights have 2^31 or more matrices, rows, or bytes or values of a row")
     if w_bytes < (K + 1) // 2 or scale.shape[-1] < (K + 31) // 32:
         raise ValueError(f"rows of {w_bytes} bytes and {scale.shape[-1]} exponents hold no {K} values")
     _dense("w", w, w.shape, torch.uint8)
