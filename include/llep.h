@@ -604,8 +604,9 @@ int32_t llep_mxfp4_row_bytes(int32_t D);
 int32_t llep_mxfp4_scale_bytes(int32_t D);
 
 /* x [R][D] in dtype to 4-bit rows: q and scale, whose rows lie q_pitch and
- * scale_pitch bytes apart (multiples of 16, at least the bytes above; a row's
- * bytes beyond those are left as they are). b = max(floor(log2 max|x|) - 2 + 127,
+ * scale_pitch bytes apart (multiples of 16, at least the bytes above and at most
+ * LLEP_MAX_FFN_DIM, here and in the calls below; a row's bytes beyond those above
+ * are left as they are). b = max(floor(log2 max|x|) - 2 + 127,
  * 1) over the block's values, which are rounded to the nearest of the grid, ties
  * to the even code, 6 at most. A block with an infinity or a NaN gets b = 255.
  * x is aligned to its type, q and scale to 16 bytes.

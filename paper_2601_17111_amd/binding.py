@@ -863,7 +863,8 @@ def _byte_rows(what: str, t, R: int, least: int, dev: int) -> int:
 
 def llep_quantize_rows_mxfp4(x, q, scale, stream=None):
     """x [R, D] (bf16 or float32) to 4-bit rows: q [R, llep_mxfp4_row_bytes(D)] and scale [R,
-    llep_mxfp4_scale_bytes(D)] uint8 (rows a multiple of 16 bytes apart)."""
+    llep_mxfp4_scale_bytes(D)] uint8 (rows a multiple of 16 bytes apart, at most
+    LLEP_MAX_FFN_DIM)."""
     R, D = x.shape
     code, _ = _type_code(x)
     at = _arguments(stream, ("x", x, (R, D), x.dtype))
