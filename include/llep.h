@@ -534,7 +534,9 @@ int llep_combine_to_bf16(const llep_plan_params *params, const float *out_perm,
  *          balancing, float32) is in the choice alone, not in the gates;
  *   groups E experts are `groups` ranges of E / groups; a group's score is its
  *          largest key or (LLEP_GROUP_TOP2) the sum of its two largest; only the
- *          experts of the top_groups best groups remain;
+ *          experts of the top_groups best groups remain. With top_groups == groups
+ *          all of them do: groups have no score then, and keys are those without
+ *          groups (l[e] where no bias is given);
  *   ids    the K experts with the largest keys, in descending order;
  *   gates  scale * s[id], or with `renormalize` scale * s[id] over the sum of
  *          the chosen experts' scores (computed relative to the largest of them,

@@ -113,8 +113,9 @@ class Router:
 
     score "softmax" or "sigmoid"; bias [E] float32 (of load balancing) or None, in the choice
     alone; groups of experts of which the top_groups best are chosen from, by their best expert
-    ("max") or the sum of their two best ("top2"); gates renormalized over the chosen experts, times
-    scale. ids and gates are this object's buffers, the current stream's as in LLEPLayer.
+    ("max") or the sum of their two best ("top2"), where top_groups is not all of them; gates
+    renormalized over the chosen experts, times scale. ids and gates are this object's buffers, the
+    current stream's as in LLEPLayer.
     """
 
     def __init__(self, T: int, K: int, E: int, score: str = "softmax", bias=None, groups: int = 1,

@@ -166,3 +166,23 @@ def test_groups_of_nothing_but_scores_of_zero(dev, low):
                     [low, -inf, -inf, low, low, low]):
             _same_ids(dev, np.repeat([row], T, 0), 4, score="sigmoid", groups=3, top_groups=2,
                       group_score="top2")
+
+
+@gpu
+@pytest.mark.parametrize("by", ["max", "top2"])
+def test_all_groups_are_no_groups(dev, by):
+    """Sigmoids that are 1 in float64 tie as keys, their logits do not: the keys are the logits where
+    every group remains, and the scores where one does not."""
+    import torch
+    l = np.repeat([[50.0, 60.0, 70.0, 80.0, 0.0, 90.0, 1.0, 2.0]], 3, 0)
+    for top in (1, 2, 4):
+        _same_ids(dev, l, 2, score="sigmoid", groups=4, top_groups=top, group_score=by)
+    from paper_2601_17111_amd import binding as B
+    x = torch.from_numpy(l).float().to(dev)
+    ids = [torch.empty((3, 2), dtype=torch.int32, device=dev) for _ in range(3)]
+    for i, (groups, top) in zip(ids, ((4, 4), (1, 1), (4, 3))):
+        B.llep_route(B.make_route(3, 2, 8, "sigmoid", groups, top, by), x, None, i,
+                     torch.empty((3, 2), device=dev))
+    assert ids[0].tolist() == ids[1].tolist() == [[5, 3]] * 3
+    # (the groups' scores are 2, 2, 1.5 and about 1.6 in float64, or 60, 80, 90 and 2)
+    assert ids[2].tolist() == ([[0, 1]] if by == "top2" else [[5, 3]]) * 3
