@@ -127,6 +127,7 @@ class Router:
         self.bias = bias
         self.ids = torch.empty((T, K), dtype=torch.int32, device=device)
         self.gates = torch.empty((T, K), dtype=torch.float32, device=device)
+        self.buffers = {}  # of backward(), by type
 
     def forward(self, logits, stream=None):
         """(ids [T, K] int32, gates [T, K] float32) for logits [T, E] (bf16 or float32)."""
@@ -134,13 +135,16 @@ class Router:
         return self.ids, self.gates
 
     def backward(self, logits, d_gates, stream=None):
-        """d_logits [T, E] of the last forward(), whose logits these are, in their type."""
-        if getattr(self, "d_logits", None) is None or self.d_logits.dtype != logits.dtype:
-            self.d_logits = B._empty((self.params.T, self.params.E), logits.dtype, logits.device,
-                                     stream)
-        B.llep_route_backward(self.params, logits, self.ids, self.gates, d_gates, self.d_logits,
-                              stream)
-        return self.d_logits
+        """d_logits [T, E] of the last forward(), whose logits these are, in their type: a buffer of
+        this object, one for each type."""
+        out = self.buffers.get(logits.dtype)
+        if out is None:
+            B._dtype_code(logits)
+            out = self.buffers[logits.dtype] = B._empty((self.params.T, self.params.E), logits.dtype,
+                                                        self.ids.device, stream)
+        B.llep_route_backward(self.params, logits, self.ids, self.gates, d_gates, out, stream)
+        self.d_logits = out
+        return out
 
 
 class LLEPLayer:
