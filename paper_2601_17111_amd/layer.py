@@ -183,7 +183,7 @@ class LLEPLayer:
         B.llep_plan(self.params, ids, self.bufs, stream)
 
     def permute(self, ids, gates, x, stream=None):
-        self.rows_are_int8 = False
+        self.rows_replaced = False
         B.llep_permute(self.params, self.bufs, ids, gates, x, self.x_perm, self.gate_perm,
                        self.row_pair, self.pair_row, stream)
 
@@ -252,7 +252,7 @@ class LLEPLayer:
             B.llep_quantize_rows(x, self.x_q, self.x_scale, stream)
             x, x_scale = self.x_q, self.x_scale
         self.gate_up_device = None
-        self.rows_are_int8 = True  # x_perm holds no rows of this call
+        self.rows_replaced = True  # x_perm holds no rows of this call
         self.plan(ids, stream)
         self._permute_int8(ids, gates, x, stream)
         B.llep_grouped_ffn_int8(self.params, self.bufs, device, self.x_perm_q, x_scale,
@@ -311,7 +311,7 @@ class LLEPLayer:
         B.llep_quantize_rows_mxfp4(x, self.x_mx[:, :self.mx_values], self.x_mx[:, self.mx_values:],
                                    stream)
         self.gate_up_device = None
-        self.rows_are_int8 = True  # x_perm holds no rows of this call
+        self.rows_replaced = True  # x_perm holds no rows of this call
         self.plan(ids, stream)
         B.llep_permute(self.params, self.bufs, ids, gates, self.x_mx.view(torch.bfloat16),
                        self.x_perm_mx.view(torch.bfloat16), self.gate_perm, self.row_pair,
@@ -340,7 +340,7 @@ class LLEPLayer:
 
     def check_backward(self):
         """Refuses a backward() whose rows forward_int8() or forward_mxfp4() has replaced."""
-        if getattr(self, "rows_are_int8", False):
+        if getattr(self, "rows_replaced", False):
             raise RuntimeError("backward() after forward_int8() or forward_mxfp4()")
 
     def backward(self, dy, gates, w_gate_up, w_gate_up_t, w_down_t, device: int = -1,
