@@ -12,12 +12,12 @@
 // with words next to each other, requested as words or written by the scale waves,
 // the products took 3 to 6% longer.)
 //
-// What bounds them: 8192^3 takes 258 us, 4.3 PFLOP/s; the matrix instructions are at
-// work 61% of the time, at the 1.6 GHz that the chip's power leaves (of 2.4: matrix
-// instructions alone, on random operands, reach 6.2 PFLOP/s). A tile's epilogue is
-// 4.5 us of 21 (K = 2048). Requests into the L2 four to eight slices further ahead made
-// products 5 to 10% slower, half tiles in a last round that leaves workgroups idle were
-// no faster.
+// What bounds them: 8192^3 takes 258 to 274 us by the card, 4.0 to 4.3 PFLOP/s; the
+// matrix instructions are at work 61% of the time, at the 1.6 GHz that the chip's power
+// leaves (of 2.4: matrix instructions alone, on random operands, reach 6.2 PFLOP/s). A
+// tile's epilogue is 4.5 us of 21 (K = 2048). Requests into the L2 four to eight slices
+// further ahead made products 5 to 10% slower, half tiles in a last round that leaves
+// workgroups idle were no faster.
 #pragma once
 
 #include "gemm.h"
